@@ -225,6 +225,74 @@ int kimad_apply_packed(const kimad_ctx* ctx, const kimad_packed* msg, float* est
 int kimad_aggregate(float* x_dev, const float* est_dev, uint64_t stride, uint32_t n_workers, uint64_t n,
                     const float* weights, float gamma, void* cuda_stream);
 
+/* ---- Microscaled 4-bit floats: the quantising compressor beside TopK, and products of quantised matrices ----------
+ *
+ * Format.  32 consecutive values are a block with one scale, a power of two; the values are held as E2M1 (sign, two exponent bits, one of
+ * mantissa: 0, .5, 1, 1.5, 2, 3, 4, 6 scales).  Scale byte s, scale 2^(s - 127): s = max(E - 2, 0) with E the binary32 exponent field
+ * of the block's largest magnitude.  Values go to the nearest multiple, ties to the even code, and end at 6 scales (a largest
+ * magnitude of 6 to 8 scales is cut).  The code's bit 3 is the sign; the even value of two is in the low half of their byte.  A block with Inf or
+ * NaN has s = 255 and codes 0.
+ *
+ * Messages.  Every layer is cut into blocks of its own, the last one filled up with zeros: ceil(n_l / 32) blocks, 16 bytes of codes
+ * and one of scale each, layers in list order.  Of a worker: codes of code_bytes, scales of scale_bytes (kimad_mx4_message_bytes; the last
+ * up to 15 bytes of scales are padding and not written).  The message of a layer takes 17 bytes for 32 elements whatever its values,
+ * about an eighth of the dense f32 bytes: whether it fits a budget is known without a search (compare with kimad_plan_budget's c).
+ * Device memory of the caller's, all workers behind each other:
+ *   codes   u8 [W][code_bytes], scales u8 [W][scale_bytes]  both 16-byte aligned
+ *   err     f32 [W][L]  ||d_l - C(d_l)||^2, summed in binary64; may be NULL where the message is only read
+ *   stats   [W]         used_bytes = 17 bytes per block, n_selected = N, budget_bytes = 0 (no budget is taken); may be NULL likewise
+ * The same contexts as for TopK, of any policy, with their workspace attached; the ratio grid and D play no role.  Steps of either kind may
+ * follow each other on the same estimators. */
+enum { KIMAD_F32 = 0, KIMAD_BF16 = 1, KIMAD_F16 = 2 }; /* element types of the calls below */
+typedef struct {
+    uint8_t* codes;
+    uint8_t* scales;
+    float* err;
+    kimad_stats* stats;
+} kimad_mx4_message;
+
+/* Bytes of one worker's message (either pointer may be NULL).  Host-only.  Errors: INVALID_ARG. */
+int kimad_mx4_message_bytes(const kimad_ctx* ctx, uint64_t* code_bytes, uint64_t* scale_bytes);
+
+/* The compression pass with C = the 4-bit quantiser: d = fl32(grad - g), message, g <- fl32(g + C(d)) (binary32, as kimad_apply_packed's adds).
+ *   grads_dev  device, of grad_dtype (KIMAD_F32, KIMAD_BF16, KIMAD_F16), [W][worker_stride], read only
+ *   state_dev  device, f32 [W][worker_stride], updated in place; must not overlap grads
+ * An absent block (d is Inf or NaN somewhere in it) sends nothing: the estimator keeps its 32 values, the layer's err and the worker's
+ * total_err are Inf, and with check_finite the worker's status is KIMAD_ERR_NONFINITE (its other blocks are sent).  Asynchronous on
+ * cuda_stream, capturable, no synchronisation; any alignment of the elements (same speed).  Uses the context's workspace: as with
+ * kimad_step, calls on one context follow each other on one stream.  Errors: INVALID_ARG, WORKSPACE, CUDA. */
+int kimad_mx4_step(kimad_ctx* ctx, const void* grads_dev, uint32_t grad_dtype, float* state_dev, const kimad_mx4_message* out, void* cuda_stream);
+
+/* The receiving side: est_m <- fl32(est_m + C_m) for every worker m (absent blocks leave est_m as it is), so that a receiver's copy stays
+ * bit-identical to the sender's state.  With x_dev also the model step over the updated estimators, x <- x - gamma sum_m w_m est_m, in
+ * the same pass and with the roundings of kimad_aggregate; weights: HOST f32 [W], W up to KIMAD_MAX_AGG_WORKERS.  x_dev NULL: weights and
+ * gamma are not looked at.  est_dev: device f32 [W][worker_stride], in place; x_dev: device f32 [N], in place.  msg may be any bytes: they
+ * decide values, not addresses.  Asynchronous on cuda_stream.  Errors: INVALID_ARG, WORKSPACE, CUDA. */
+int kimad_mx4_apply(const kimad_ctx* ctx, const kimad_mx4_message* msg, float* est_dev, float* x_dev, const float* weights, float gamma,
+                    void* cuda_stream);
+
+/* The message as dense values, out_dev [W][worker_stride] of dtype (KIMAD_F32 or KIMAD_BF16, which holds them all exactly): for a collective that
+ * adds them, or a check.  Absent blocks read as 0; what lies behind N is left as it is.  Errors: INVALID_ARG, WORKSPACE, CUDA. */
+int kimad_mx4_read(const kimad_ctx* ctx, const kimad_mx4_message* msg, void* out_dev, uint32_t dtype, void* cuda_stream);
+
+/* ---- Operands: matrices quantised with blocks along one axis.  An operand has `lines` lines of `length` values, blocks along the line.
+ *   codes   u8 [batch][lines][16 ceil(length / 32)]                             16-byte aligned
+ *   scales  u8 [batch][ceil(lines / 128)][ceil(length / 128)][512]              16-byte aligned; line r and block b of a tile (128 lines by
+ *           4 blocks) at byte (r mod 32) 16 + (r div 32) 4 + b; 0 for lines and blocks that are not there
+ * lines and length at most 2^30, tiles of a batch below 2^31.
+ * kimad_mx4_operand_bytes: of one matrix of the batch.  Host-only.
+ * kimad_mx4_quantize: x_dev [batch][rows][cols] of dtype, `ld` elements from row to row (ld >= cols) and batch_stride from matrix to matrix
+ *   (0: the same one).  along 0: blocks run over the rows, the operand has `cols` lines of `rows` values (x is transposed: tokens by
+ *   features become features of tokens); along 1: blocks run over the columns, `rows` lines of `cols` values.
+ * kimad_mx4_dequantize: back to values, dtype KIMAD_F32 or KIMAD_BF16 (exact in both); blocks of scale 255 read as NaN.  What lies between the rows is left
+ *   as it is; matrices of a batch must not overlap.
+ * rows, cols or batch 0: nothing is done.  Asynchronous on cuda_stream; no context, no workspace.  Errors: INVALID_ARG, CUDA. */
+int kimad_mx4_operand_bytes(uint64_t lines, uint64_t length, uint64_t* code_bytes, uint64_t* scale_bytes);
+int kimad_mx4_quantize(const void* x_dev, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t batch, uint64_t batch_stride, uint32_t along,
+                       uint8_t* codes_dev, uint8_t* scales_dev, void* cuda_stream);
+int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, void* x_dev, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld,
+                         uint64_t batch, uint64_t batch_stride, uint32_t along, void* cuda_stream);
+
 /* ---- Bandwidth monitor (Section 2.4: every device estimates its bandwidth B_m^k from what it observed; the
  * paper gives no formula, this is ours).  Host-only, no GPU.  The caller reports every finished transfer (the
  * upload of a step's message: its bytes and how long it took); the estimate is the throughput over the last

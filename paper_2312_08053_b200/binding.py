@@ -43,6 +43,12 @@ class kimad_packed(C.Structure):
                 ("j", C.c_void_p), ("stats", C.c_void_p), ("dense", C.c_void_p)]
 
 
+class kimad_mx4_message(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("err", C.c_void_p), ("stats", C.c_void_p)]
+
+
+KIMAD_F32, KIMAD_BF16, KIMAD_F16 = 0, 1, 2
+
 STATS_DTYPE = np.dtype([("budget_bytes", "<u8"), ("used_bytes", "<u8"), ("n_selected", "<u8"),
                         ("total_err", "<f4"), ("status", "<i4")])
 
@@ -125,6 +131,20 @@ def load():
     L.kimad_debug_check.argtypes = [vp, C.POINTER(u32), C.POINTER(u32)]
     L.kimad_launch_count.restype = u64
     L.kimad_launch_count.argtypes = [vp]
+    L.kimad_mx4_message_bytes.restype = C.c_int
+    L.kimad_mx4_message_bytes.argtypes = [vp, C.POINTER(u64), C.POINTER(u64)]
+    L.kimad_mx4_step.restype = C.c_int
+    L.kimad_mx4_step.argtypes = [vp, vp, u32, vp, C.POINTER(kimad_mx4_message), vp]
+    L.kimad_mx4_apply.restype = C.c_int
+    L.kimad_mx4_apply.argtypes = [vp, C.POINTER(kimad_mx4_message), vp, vp, C.POINTER(C.c_float), C.c_float, vp]
+    L.kimad_mx4_read.restype = C.c_int
+    L.kimad_mx4_read.argtypes = [vp, C.POINTER(kimad_mx4_message), vp, u32, vp]
+    L.kimad_mx4_operand_bytes.restype = C.c_int
+    L.kimad_mx4_operand_bytes.argtypes = [u64, u64, C.POINTER(u64), C.POINTER(u64)]
+    L.kimad_mx4_quantize.restype = C.c_int
+    L.kimad_mx4_quantize.argtypes = [vp, u32, u64, u64, u64, u64, u64, u32, vp, vp, vp]
+    L.kimad_mx4_dequantize.restype = C.c_int
+    L.kimad_mx4_dequantize.argtypes = [vp, vp, vp, u32, u64, u64, u64, u64, u64, u32, vp]
     L.kimad_monitor_create.restype = C.c_int
     L.kimad_monitor_create.argtypes = [C.POINTER(vp), u32, dbl]
     L.kimad_monitor_destroy.restype = None
@@ -403,6 +423,157 @@ def new_context(layer_sizes, n_workers, ratio_grid, device="cuda", **opts):
     kimad_set_workspace(ctx, ws[off:])
     ctx._keep.append(ws)
     return ctx
+
+
+def _mx4_dtype(t, what, names=("float32", "bfloat16", "float16")):
+    name = str(t.dtype).replace("torch.", "")
+    if name not in names:
+        raise TypeError(f"{what}: {name}, not one of {', '.join(names)}")
+    return {"float32": KIMAD_F32, "bfloat16": KIMAD_BF16, "float16": KIMAD_F16}[name]
+
+
+def _mx4_here(what, *tensors):
+    """The library takes memory of the current device (a tensor of another one is refused, as is one in host memory)."""
+    import torch
+
+    for t in tensors:
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{what}: tensor on {t.device}, not on the current CUDA device")
+
+
+def _mx4_workers(ctx, t, what):
+    if t.dim() != 2 or t.shape[0] != ctx.W or t.shape[1] < ctx.N or (t.shape[1] > 1 and t.stride(1) != 1) or (ctx.W > 1 and t.stride(0) != ctx.stride):
+        raise ValueError(f"{what}: [{ctx.W}][{ctx.stride}] with rows of consecutive elements, not {tuple(t.shape)} with strides {t.stride()}")
+
+
+def kimad_mx4_message_bytes(ctx: Ctx):
+    """(bytes of codes, bytes of scales) of one worker's 4-bit message."""
+    c, s = C.c_uint64(0), C.c_uint64(0)
+    _check(load().kimad_mx4_message_bytes(ctx.handle, C.byref(c), C.byref(s)), "kimad_mx4_message_bytes")
+    return int(c.value), int(s.value)
+
+
+class Mx4Message:
+    """Device buffers of all workers' 4-bit messages and the matching ``kimad_mx4_message`` struct."""
+
+    def __init__(self, ctx: Ctx, device="cuda"):
+        import torch
+
+        code_bytes, scale_bytes = kimad_mx4_message_bytes(ctx)
+        self.codes = torch.zeros((ctx.W, code_bytes), dtype=torch.uint8, device=device)
+        self.scales = torch.zeros((ctx.W, scale_bytes), dtype=torch.uint8, device=device)
+        self.err = torch.zeros((ctx.W, ctx.L), dtype=torch.float32, device=device)
+        self.stats = torch.zeros((ctx.W, STATS_DTYPE.itemsize), dtype=torch.uint8, device=device)
+        self.c = kimad_mx4_message(self.codes.data_ptr(), self.scales.data_ptr(), self.err.data_ptr(), self.stats.data_ptr())
+
+    def stats_host(self) -> np.ndarray:
+        return self.stats.cpu().numpy().view(STATS_DTYPE).reshape(-1)
+
+
+def _mx4_message(ctx, msg, what):
+    """The struct of a message, whose buffers have to be those of a context of this shape."""
+    code_bytes, scale_bytes = kimad_mx4_message_bytes(ctx)
+    if tuple(msg.codes.shape) != (ctx.W, code_bytes) or tuple(msg.scales.shape) != (ctx.W, scale_bytes) or tuple(msg.err.shape) != (ctx.W, ctx.L):
+        raise ValueError(f"{what}: a message of another context's shape")
+    _mx4_here(what, msg.codes)
+    return C.byref(msg.c)
+
+
+def kimad_mx4_step(ctx: Ctx, grads, state, msg: Mx4Message, stream=None) -> None:
+    """grads: CUDA float32, bfloat16 or float16 [W][ctx.stride]; state: CUDA float32 of that shape, updated in place."""
+    dtype = _mx4_dtype(grads, "grads")
+    _mx4_dtype(state, "state", ("float32",))
+    for t, what in ((grads, "grads"), (state, "state")):
+        _mx4_workers(ctx, t, what)
+    m = _mx4_message(ctx, msg, "kimad_mx4_step")
+    _mx4_here("kimad_mx4_step", grads, state)
+    _check(load().kimad_mx4_step(ctx.handle, grads.data_ptr(), dtype, state.data_ptr(), m, _stream_ptr(stream)), "kimad_mx4_step")
+
+
+def kimad_mx4_apply(ctx: Ctx, msg: Mx4Message, est, x=None, weights=None, gamma=0.0, stream=None) -> None:
+    """est: CUDA float32 [W][ctx.stride], in place.  With x (CUDA float32 [N], in place) also the model step: weights, W host floats, and gamma."""
+    _mx4_dtype(est, "est", ("float32",))
+    _mx4_workers(ctx, est, "est")
+    m = _mx4_message(ctx, msg, "kimad_mx4_apply")
+    _mx4_here("kimad_mx4_apply", est)
+    if x is None:
+        _check(load().kimad_mx4_apply(ctx.handle, m, est.data_ptr(), None, None, C.c_float(0.0), _stream_ptr(stream)), "kimad_mx4_apply")
+        return
+    _mx4_dtype(x, "x", ("float32",))
+    w = np.ascontiguousarray([] if weights is None else weights, dtype=np.float32).reshape(-1)
+    if w.size != ctx.W or x.dim() != 1 or x.numel() != ctx.N or (ctx.N > 1 and x.stride(0) != 1):
+        raise ValueError(f"kimad_mx4_apply: x of {ctx.N} consecutive elements and {ctx.W} weights")
+    _mx4_here("kimad_mx4_apply", x)
+    _check(load().kimad_mx4_apply(ctx.handle, m, est.data_ptr(), x.data_ptr(), w.ctypes.data_as(C.POINTER(C.c_float)), C.c_float(gamma),
+                                  _stream_ptr(stream)), "kimad_mx4_apply")
+
+
+def kimad_mx4_read(ctx: Ctx, msg: Mx4Message, out, stream=None) -> None:
+    """out: CUDA float32 or bfloat16 [W][ctx.stride], the values that the messages stand for."""
+    dtype = _mx4_dtype(out, "out", ("float32", "bfloat16"))
+    _mx4_workers(ctx, out, "out")
+    m = _mx4_message(ctx, msg, "kimad_mx4_read")
+    _mx4_here("kimad_mx4_read", out)
+    _check(load().kimad_mx4_read(ctx.handle, m, out.data_ptr(), dtype, _stream_ptr(stream)), "kimad_mx4_read")
+
+
+def kimad_mx4_operand_bytes(lines: int, length: int):
+    """(bytes of codes, bytes of scales) of one quantised matrix of ``lines`` lines of ``length`` values."""
+    c, s = C.c_uint64(0), C.c_uint64(0)
+    _check(load().kimad_mx4_operand_bytes(lines, length, C.byref(c), C.byref(s)), "kimad_mx4_operand_bytes")
+    return int(c.value), int(s.value)
+
+
+class Mx4Operand:
+    """``batch`` matrices of ``lines`` lines of ``length`` values, quantised along their lines (see kimad.h for the layout): new device buffers, or
+    those of a message that has arrived."""
+
+    def __init__(self, lines: int, length: int, batch: int = 1, codes=None, scales=None, device="cuda"):
+        import torch
+
+        self.lines, self.length, self.batch = int(lines), int(length), int(batch)
+        code_bytes, scale_bytes = kimad_mx4_operand_bytes(self.lines, self.length)
+        self.codes = torch.empty((batch, code_bytes), dtype=torch.uint8, device=device) if codes is None else codes
+        self.scales = torch.empty((batch, scale_bytes), dtype=torch.uint8, device=device) if scales is None else scales
+        for t, n in ((self.codes, code_bytes), (self.scales, scale_bytes)):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != batch * n:
+                raise ValueError(f"an operand of {batch} x {lines} x {length} has {batch * n} contiguous bytes, not {tuple(t.shape)} of {t.dtype}")
+
+
+def _mx4_matrix(t, op, along, what):
+    """(batch, rows, cols, row stride, matrix stride) of a [rows][cols] or [batch][rows][cols] tensor that goes with an operand."""
+    if t.dim() == 2:
+        t = t[None]
+    if t.dim() != 3 or along not in (0, 1):
+        raise ValueError(f"{what}: [rows][cols] or [batch][rows][cols], along 0 or 1")
+    b, rows, cols = t.shape
+    if (b, rows, cols) != (op.batch, *((op.length, op.lines) if along == 0 else (op.lines, op.length))):
+        raise ValueError(f"{what}: {tuple(t.shape)} along {along} is not an operand of {op.batch} x {op.lines} x {op.length}")
+    if cols > 1 and t.stride(2) != 1:
+        raise ValueError(f"{what}: columns have to be consecutive elements, not {t.stride(2)} apart")
+    ld = t.stride(1) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap")
+    return b, rows, cols, ld, t.stride(0) if b > 1 else 0
+
+
+def kimad_mx4_quantize(x, op: Mx4Operand, along: int, stream=None) -> None:
+    """x: CUDA float32, bfloat16 or float16, [rows][cols] or [batch][rows][cols].  along 0: blocks over the rows (the operand is x transposed), 1: over
+    the columns."""
+    dtype = _mx4_dtype(x, "x")
+    b, rows, cols, ld, bs = _mx4_matrix(x, op, along, "x")
+    _mx4_here("kimad_mx4_quantize", x, op.codes, op.scales)
+    _check(load().kimad_mx4_quantize(x.data_ptr(), dtype, rows, cols, ld, b, bs, along, op.codes.data_ptr(), op.scales.data_ptr(), _stream_ptr(stream)),
+           "kimad_mx4_quantize")
+
+
+def kimad_mx4_dequantize(op: Mx4Operand, out, along: int, stream=None) -> None:
+    """out: CUDA float32 or bfloat16, shaped as kimad_mx4_quantize's x."""
+    dtype = _mx4_dtype(out, "out", ("float32", "bfloat16"))
+    b, rows, cols, ld, bs = _mx4_matrix(out, op, along, "out")
+    _mx4_here("kimad_mx4_dequantize", out, op.codes, op.scales)
+    _check(load().kimad_mx4_dequantize(op.codes.data_ptr(), op.scales.data_ptr(), out.data_ptr(), dtype, rows, cols, ld, b, bs, along, _stream_ptr(stream)),
+           "kimad_mx4_dequantize")
 
 
 class Monitor:

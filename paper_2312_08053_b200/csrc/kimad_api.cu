@@ -7,11 +7,13 @@
 #include <cstdio>
 #include <cstring>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "kimad_dp.cuh"
 #include "kimad_select.cuh"
 #include "kimad_receiver.cuh"
+#include "kimad_mx4.cuh"
 
 using namespace kimad;
 
@@ -49,6 +51,7 @@ struct kimad_ctx {
     std::vector<size_t> guards;                               // checked build: offsets of the canary words between regions
     uint32_t most_chunks = 0; // of a layer
     uint64_t most_elems = 0;
+    uint64_t blocks = 0; // of 32 elements, of a worker's 4-bit message
     uint32_t sample_ctas = 1; // that read a layer's sample together (prepare_device)
     bool odd = false;         // workers may start at different distances from a 128-bit boundary
     uint32_t curve_mode = 0;
@@ -183,6 +186,8 @@ static int preload_kernels() {
     KIMAD_PRELOAD((k_sel_write<true, false>)); KIMAD_PRELOAD((k_sel_write<true, true>));
     KIMAD_PRELOAD(k_apply_packed<false>); KIMAD_PRELOAD(k_apply_packed<true>);
     KIMAD_PRELOAD(k_aggregate<false>); KIMAD_PRELOAD(k_aggregate<true>);
+    KIMAD_PRELOAD(k_mx4_step<float>); KIMAD_PRELOAD(k_mx4_step<__nv_bfloat16>); KIMAD_PRELOAD(k_mx4_step<__half>); KIMAD_PRELOAD(k_mx4_stats);
+    KIMAD_PRELOAD(k_mx4_apply<false>); KIMAD_PRELOAD(k_mx4_apply<true>); KIMAD_PRELOAD(k_mx4_read<float>); KIMAD_PRELOAD(k_mx4_read<__nv_bfloat16>);
 #undef KIMAD_PRELOAD
     return KIMAD_OK;
 }
@@ -698,7 +703,7 @@ int kimad_create(kimad_ctx** out, const uint64_t* layer_sizes, uint32_t n_layers
             LayerDesc ld{N, n, (uint32_t)c->chunks.size(), 0};
             for (uint64_t p = N; p < N + n;) {
                 const uint64_t e = std::min(N + n, (p / window + 1) * window);
-                c->chunks.push_back(Chunk{l, 0, p, e});
+                c->chunks.push_back(Chunk{l, (uint32_t)(c->blocks + (p - N + kMxBlock - 1) / kMxBlock), p, e});
                 p = e;
             }
             ld.n_chunks = (uint32_t)c->chunks.size() - ld.first_chunk;
@@ -712,6 +717,7 @@ int kimad_create(kimad_ctx** out, const uint64_t* layer_sizes, uint32_t n_layers
                 c->reg_index.push_back((uint32_t)c->reg_layers.size());
                 c->reg_layers.push_back(l);
             }
+            c->blocks += (n + kMxBlock - 1) / kMxBlock;
             N += n;
         }
         c->N = N;
@@ -1083,6 +1089,160 @@ int kimad_debug_check(kimad_ctx* c, uint32_t* failed_checks, uint32_t* damaged_c
 }
 
 uint64_t kimad_launch_count(const kimad_ctx* ctx) { return ctx ? ctx->launches : 0; }
+
+// ---------------------------------------------------------------------------------------------------
+// 4-bit messages and operands (kimad_mx4.cuh)
+// ---------------------------------------------------------------------------------------------------
+} // extern "C"
+namespace {
+
+static_assert(sizeof(ChunkSel) >= kMxPieces * sizeof(MxPartial), "the sums of a chunk's CTAs lie where the selection keeps its counts");
+
+// CTAs per chunk, as a power of two: a chunk takes a CTA sixteen rounds of its warps, so a context of few chunks spreads them until every SM
+// has eight CTAs.
+uint32_t mx4_log_pieces(uint64_t chunks) {
+    uint32_t lp = 0;
+    while ((1u << lp) < kMxPieces && (chunks << lp) < 148 * 8) ++lp;
+    return lp;
+}
+uint64_t mx4_code_bytes(const kimad_ctx* c) { return c->blocks * 16; }
+uint64_t mx4_scale_bytes(const kimad_ctx* c) { return (c->blocks + 15) / 16 * 16; }
+bool mx4_message_ok(const kimad_ctx* c, const kimad_mx4_message* m) {
+    return c && m && m->codes && m->scales && (uintptr_t)m->codes % 16 == 0 && (uintptr_t)m->scales % 16 == 0 && c->blocks <= 0xffffffffull &&
+           c->W <= 65535;
+}
+
+// What the calls on matrices check: 0 < lines, length <= 2^30, buffers on 16 bytes, tiles within a grid.
+constexpr uint64_t kMxMostLines = 1ull << 30;
+bool mx4_operand_ok(uint64_t lines, uint64_t length, uint64_t batch, const void* codes, const void* scales) {
+    if (lines > kMxMostLines || length > kMxMostLines || (uintptr_t)codes % 16 || (uintptr_t)scales % 16) return false;
+    const MxOperand op((uint32_t)lines, (uint32_t)length);
+    const uint64_t tiles = (uint64_t)op.line_tiles * op.block_tiles;
+    return tiles <= 0x7fffffffull && (tiles == 0 || batch <= 0x7fffffffull / tiles);
+}
+
+} // namespace
+extern "C" {
+
+int kimad_mx4_message_bytes(const kimad_ctx* c, uint64_t* code_bytes, uint64_t* scale_bytes) {
+    if (!c) return KIMAD_ERR_INVALID_ARG;
+    if (code_bytes) *code_bytes = mx4_code_bytes(c);
+    if (scale_bytes) *scale_bytes = mx4_scale_bytes(c);
+    return KIMAD_OK;
+}
+
+int kimad_mx4_step(kimad_ctx* c, const void* grads_dev, uint32_t grad_dtype, float* state_dev, const kimad_mx4_message* out, void* cuda_stream) {
+    if (!mx4_message_ok(c, out) || !out->err || !out->stats || !grads_dev || !state_dev || grad_dtype > KIMAD_F16 ||
+        (uintptr_t)grads_dev % (grad_dtype == KIMAD_F32 ? 4 : 2) || (uintptr_t)state_dev % 4)
+        return KIMAD_ERR_INVALID_ARG;
+    if (!c->ws) return KIMAD_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const uint32_t nch = (uint32_t)c->chunks.size(), lp = mx4_log_pieces((uint64_t)nch * c->W);
+    const Chunk* chunks = c->at<Chunk>(c->lay.chunks);
+    const LayerDesc* layers = c->at<LayerDesc>(c->lay.layers);
+    MxPartial* partial = c->at<MxPartial>(c->lay.csel); // (the selection of a TopK step is over when this runs, and starts from its own counts)
+    auto launch = [&](auto kern, auto* grads) {
+        return launch_named("k_mx4_step", kern, dim3(nch << lp, c->W), kThreads, 0, s, grads, state_dev, c->stride, chunks, layers, lp, out->codes,
+                            out->scales, mx4_code_bytes(c), mx4_scale_bytes(c), partial);
+    };
+    CUDA_TRY(grad_dtype == KIMAD_F32 ? launch(k_mx4_step<float>, static_cast<const float*>(grads_dev))
+             : grad_dtype == KIMAD_BF16 ? launch(k_mx4_step<__nv_bfloat16>, static_cast<const __nv_bfloat16*>(grads_dev))
+                                        : launch(k_mx4_step<__half>, static_cast<const __half*>(grads_dev)));
+    CUDA_TRY(launch_pdl(k_mx4_stats, c->W, kMxStatsThreads, 0, s, partial, layers, c->L, nch, lp, c->N, c->blocks * 17, c->check_finite, out->err,
+                        out->stats));
+    c->launches += 2;
+    CUDA_TRY(cudaGetLastError());
+    return KIMAD_OK;
+}
+
+int kimad_mx4_apply(const kimad_ctx* c, const kimad_mx4_message* msg, float* est_dev, float* x_dev, const float* weights, float gamma, void* cuda_stream) {
+    if (!mx4_message_ok(c, msg) || !est_dev || (uintptr_t)est_dev % 4 || (x_dev && (!weights || c->W > KIMAD_MAX_AGG_WORKERS || (uintptr_t)x_dev % 4)))
+        return KIMAD_ERR_INVALID_ARG;
+    if (!c->ws) return KIMAD_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const uint32_t nch = (uint32_t)c->chunks.size(), rows = x_dev ? 1u : c->W, lp = mx4_log_pieces((uint64_t)nch * rows);
+    MxWeights wt{};
+    for (uint32_t m = 0; x_dev && m < c->W; ++m) wt.w[m] = weights[m];
+    auto launch = [&](auto kern) {
+        return launch_named("k_mx4_apply", kern, dim3(nch << lp, rows), kThreads, 0, s, msg->codes, msg->scales, mx4_code_bytes(c), mx4_scale_bytes(c),
+                            c->at<const Chunk>(c->lay.chunks), c->at<const LayerDesc>(c->lay.layers), lp, est_dev, c->stride, c->W, x_dev, wt, gamma);
+    };
+    CUDA_TRY(x_dev ? launch(k_mx4_apply<true>) : launch(k_mx4_apply<false>));
+    CUDA_TRY(cudaGetLastError());
+    return KIMAD_OK;
+}
+
+int kimad_mx4_read(const kimad_ctx* c, const kimad_mx4_message* msg, void* out_dev, uint32_t dtype, void* cuda_stream) {
+    if (!mx4_message_ok(c, msg) || !out_dev || dtype > KIMAD_BF16 || (uintptr_t)out_dev % (dtype == KIMAD_F32 ? 4 : 2)) return KIMAD_ERR_INVALID_ARG;
+    if (!c->ws) return KIMAD_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const uint32_t nch = (uint32_t)c->chunks.size(), lp = mx4_log_pieces((uint64_t)nch * c->W);
+    auto launch = [&](auto kern, auto* out) {
+        return launch_named("k_mx4_read", kern, dim3(nch << lp, c->W), kThreads, 0, s, msg->codes, msg->scales, mx4_code_bytes(c), mx4_scale_bytes(c),
+                            c->at<const Chunk>(c->lay.chunks), c->at<const LayerDesc>(c->lay.layers), lp, out, c->stride);
+    };
+    CUDA_TRY(dtype == KIMAD_F32 ? launch(k_mx4_read<float>, static_cast<float*>(out_dev))
+                                : launch(k_mx4_read<__nv_bfloat16>, static_cast<__nv_bfloat16*>(out_dev)));
+    CUDA_TRY(cudaGetLastError());
+    return KIMAD_OK;
+}
+
+int kimad_mx4_operand_bytes(uint64_t lines, uint64_t length, uint64_t* code_bytes, uint64_t* scale_bytes) {
+    if (lines > kMxMostLines || length > kMxMostLines) return KIMAD_ERR_INVALID_ARG;
+    const MxOperand op((uint32_t)lines, (uint32_t)length);
+    if (code_bytes) *code_bytes = op.code_bytes();
+    if (scale_bytes) *scale_bytes = op.scale_bytes();
+    return KIMAD_OK;
+}
+
+int kimad_mx4_quantize(const void* x_dev, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t batch, uint64_t batch_stride, uint32_t along,
+                       uint8_t* codes_dev, uint8_t* scales_dev, void* cuda_stream) {
+    const uint64_t lines = along ? rows : cols, length = along ? cols : rows;
+    if (dtype > KIMAD_F16 || along > 1 || ld < cols || !mx4_operand_ok(lines, length, batch, codes_dev, scales_dev) ||
+        (uintptr_t)x_dev % (dtype == KIMAD_F32 ? 4 : 2))
+        return KIMAD_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0 || batch == 0) return KIMAD_OK;
+    if (!x_dev || !codes_dev || !scales_dev) return KIMAD_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const MxOperand op((uint32_t)lines, (uint32_t)length);
+    auto launch = [&](auto* x) {
+        using T = std::remove_cv_t<std::remove_pointer_t<decltype(x)>>;
+        if (along == 0)
+            return launch_named("k_mx4_quantize_cols", k_mx4_quantize_cols<T>, dim3((uint32_t)(batch * op.line_tiles * op.block_tiles)), kMxColThreads, 0, s, x,
+                                ld, batch_stride, op, codes_dev, scales_dev);
+        const uint64_t warps = batch * op.line_tiles * kMxTile * ((op.blocks + kMxGroup - 1) / kMxGroup);
+        return launch_named("k_mx4_quantize_rows", k_mx4_quantize_rows<T>, dim3((uint32_t)std::min<uint64_t>((warps + 7) / 8, 148 * 32)), kThreads, 0, s, x,
+                            ld, batch_stride, batch, op, codes_dev, scales_dev);
+    };
+    CUDA_TRY(dtype == KIMAD_F32 ? launch(static_cast<const float*>(x_dev))
+             : dtype == KIMAD_BF16 ? launch(static_cast<const __nv_bfloat16*>(x_dev)) : launch(static_cast<const __half*>(x_dev)));
+    CUDA_TRY(cudaGetLastError());
+    return KIMAD_OK;
+}
+
+int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, void* x_dev, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld,
+                         uint64_t batch, uint64_t batch_stride, uint32_t along, void* cuda_stream) {
+    const uint64_t lines = along ? rows : cols, length = along ? cols : rows;
+    if (dtype > KIMAD_BF16 || along > 1 || ld < cols || !mx4_operand_ok(lines, length, batch, codes_dev, scales_dev) ||
+        (uintptr_t)x_dev % (dtype == KIMAD_F32 ? 4 : 2))
+        return KIMAD_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0 || batch == 0) return KIMAD_OK;
+    if (!x_dev || !codes_dev || !scales_dev || (batch > 1 && batch_stride < (rows - 1) * ld + cols)) return KIMAD_ERR_INVALID_ARG; // outputs on top of each other
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const MxOperand op((uint32_t)lines, (uint32_t)length);
+    auto launch = [&](auto* x) {
+        using T = std::remove_pointer_t<decltype(x)>;
+        if (along == 0)
+            return launch_named("k_mx4_dequantize_cols", k_mx4_dequantize_cols<T>, dim3((uint32_t)(batch * op.line_tiles * op.block_tiles)), kMxColThreads, 0, s, x,
+                                ld, batch_stride, op, codes_dev, scales_dev);
+        const uint64_t warps = batch * op.lines * ((op.blocks + kMxGroup - 1) / kMxGroup);
+        return launch_named("k_mx4_dequantize_rows", k_mx4_dequantize_rows<T>, dim3((uint32_t)std::min<uint64_t>((warps + 7) / 8, 148 * 32)), kThreads, 0, s, x,
+                            ld, batch_stride, batch, op, codes_dev, scales_dev);
+    };
+    CUDA_TRY(dtype == KIMAD_F32 ? launch(static_cast<float*>(x_dev)) : launch(static_cast<__nv_bfloat16*>(x_dev)));
+    CUDA_TRY(cudaGetLastError());
+    return KIMAD_OK;
+}
 
 // ---------------------------------------------------------------------------------------------------
 // Bandwidth monitor: windowed throughput of the reported transfers with exponential smoothing (host only)

@@ -16,7 +16,8 @@
 // traps.  Bits: 0 sweep: bin outside the layer's histogram; 1 counting sweep: key outside its interval;
 // 2 a work list (exact path, recount) appended beyond its capacity; 3 write sweep: packed position beyond the capacity or element
 // outside its chunk; 4 knapsack: a record, row or exchange outside the memory it lies in; 5 knapsack: a cell outside its row;
-// 6 selection: a listed entry outside its layer's chunks; 7 curve: the pieces of a refined bin do not add up to the bin.
+// 6 selection: a listed entry outside its layer's chunks; 7 curve: the pieces of a refined bin do not add up to the bin; 8 4-bit message: a block
+// behind the buffers' end.
 // In the ordinary build KIMAD_CHECK(cond, bit) is `true`.
 #if defined(KIMAD_CHECKED) && defined(__CUDACC__)
 __device__ unsigned int g_kimad_check_word;
@@ -38,7 +39,7 @@ constexpr int kDpWorkersPerLaunch = 32;
 
 struct Chunk {
     uint32_t layer;
-    uint32_t _pad;
+    uint32_t block; // place in a worker's 4-bit message of the first block that starts in the chunk (kimad_mx4.cuh)
     uint64_t begin; // flat element index inside the worker's vector
     uint64_t end;
 };
