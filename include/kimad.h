@@ -293,6 +293,19 @@ int kimad_mx4_quantize(const void* x_dev, uint32_t dtype, uint64_t rows, uint64_
 int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, void* x_dev, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld,
                          uint64_t batch, uint64_t batch_stride, uint32_t along, void* cuda_stream);
 
+/* kimad_mx4_product: out <- beta out + alpha A B^T, A an operand of m lines, B one of n lines, both of `length` values: out_ij gets alpha sum_t A_it B_jt.
+ * With the two factors of a linear layer's gradient (its inputs and its outputs' gradients, quantised along the tokens: along 0) this is that
+ * gradient, summed over the tokens into the layer's place in a flat gradient or estimator vector: out_dev device f32, [batch][m][n], `ld` elements from
+ * row to row and batch_stride from matrix to matrix (no two outputs on top of each other), any alignment of elements.  The sum is
+ * taken in binary32 on the tensor cores (products of codes exactly, at most one rounding per 32 values and addition), always in the same
+ * order; then fl32(alpha sum), with beta != 0 fl32(beta out + that) with one rounding; with beta = 0 out is not read.  Blocks of scale 255 make NaN of their
+ * line's outputs.  length 0: out <- beta out.  What lies between rows and matrices is left as it is.
+ * status_dev: device i32 or NULL; set to KIMAD_ERR_TIMEOUT if a bounded wait inside the kernel ran out (its tile is then not written), else left as it is.
+ * Asynchronous on cuda_stream; no context, no workspace.  m, n or batch 0: nothing is done.  Errors: INVALID_ARG, CUDA. */
+int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64_t m, uint64_t n, uint64_t length, uint64_t batch, const uint8_t* a_codes_dev,
+                      const uint8_t* a_scales_dev, const uint8_t* b_codes_dev, const uint8_t* b_scales_dev, float alpha, float beta, int32_t* status_dev,
+                      void* cuda_stream);
+
 /* ---- Bandwidth monitor (Section 2.4: every device estimates its bandwidth B_m^k from what it observed; the
  * paper gives no formula, this is ours).  Host-only, no GPU.  The caller reports every finished transfer (the
  * upload of a step's message: its bytes and how long it took); the estimate is the throughput over the last

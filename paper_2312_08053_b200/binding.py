@@ -145,6 +145,8 @@ def load():
     L.kimad_mx4_quantize.argtypes = [vp, u32, u64, u64, u64, u64, u64, u32, vp, vp, vp]
     L.kimad_mx4_dequantize.restype = C.c_int
     L.kimad_mx4_dequantize.argtypes = [vp, vp, vp, u32, u64, u64, u64, u64, u64, u32, vp]
+    L.kimad_mx4_product.restype = C.c_int
+    L.kimad_mx4_product.argtypes = [vp] + [u64] * 6 + [vp] * 4 + [C.c_float, C.c_float, vp, vp]
     L.kimad_monitor_create.restype = C.c_int
     L.kimad_monitor_create.argtypes = [C.POINTER(vp), u32, dbl]
     L.kimad_monitor_destroy.restype = None
@@ -574,6 +576,26 @@ def kimad_mx4_dequantize(op: Mx4Operand, out, along: int, stream=None) -> None:
     _mx4_here("kimad_mx4_dequantize", out, op.codes, op.scales)
     _check(load().kimad_mx4_dequantize(op.codes.data_ptr(), op.scales.data_ptr(), out.data_ptr(), dtype, rows, cols, ld, b, bs, along, _stream_ptr(stream)),
            "kimad_mx4_dequantize")
+
+
+def kimad_mx4_product(a: Mx4Operand, b: Mx4Operand, out, alpha=1.0, beta=0.0, status=None, stream=None) -> None:
+    """out <- beta out + alpha a b^T.  out: CUDA float32 [a.lines][b.lines] or [batch][a.lines][b.lines], rows of consecutive elements at any stride
+    and place; status: CUDA int32 tensor of one element or None."""
+    _mx4_dtype(out, "out", ("float32",))
+    if (a.length, a.batch) != (b.length, b.batch):
+        raise ValueError(f"kimad_mx4_product: operands of {a.batch} x {a.length} and of {b.batch} x {b.length}")
+    o = out[None] if out.dim() == 2 else out
+    if tuple(o.shape) != (a.batch, a.lines, b.lines) or (b.lines > 1 and o.stride(2) != 1):
+        raise ValueError(f"kimad_mx4_product: out of {a.batch} x {a.lines} x {b.lines} with rows of consecutive elements, not {tuple(out.shape)}")
+    ld = o.stride(1) if a.lines > 1 else b.lines
+    if ld < b.lines:
+        raise ValueError("kimad_mx4_product: rows of out overlap")
+    _mx4_here("kimad_mx4_product", out, a.codes, a.scales, b.codes, b.scales, *(() if status is None else (status,)))
+    if status is not None and (str(status.dtype) != "torch.int32" or status.numel() < 1):
+        raise TypeError("kimad_mx4_product: status is an int32 tensor")
+    _check(load().kimad_mx4_product(out.data_ptr(), ld, o.stride(0) if a.batch > 1 else 0, a.lines, b.lines, a.length, a.batch, a.codes.data_ptr(),
+                                    a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), C.c_float(alpha), C.c_float(beta),
+                                    None if status is None else status.data_ptr(), _stream_ptr(stream)), "kimad_mx4_product")
 
 
 class Monitor:

@@ -14,6 +14,7 @@ HEADERS = [os.path.join(_HERE, "csrc", "kimad_kernels.cuh"), os.path.join(_HERE,
            os.path.join(_HERE, "csrc", "kimad_curve.cuh"), os.path.join(_HERE, "csrc", "kimad_common.h"),
            os.path.join(_HERE, "csrc", "kimad_receiver.cuh"), os.path.join(_HERE, "csrc", "kimad_dp.cuh"),
            os.path.join(_HERE, "csrc", "kimad_dp_window.cuh"), os.path.join(_HERE, "csrc", "kimad_mx4.cuh"),
+           os.path.join(_HERE, "csrc", "kimad_mx4_product.cuh"),
            os.path.join(_ROOT, "include", "kimad.h")]
 
 

@@ -14,6 +14,7 @@
 #include "kimad_select.cuh"
 #include "kimad_receiver.cuh"
 #include "kimad_mx4.cuh"
+#include "kimad_mx4_product.cuh"
 
 using namespace kimad;
 
@@ -1121,6 +1122,30 @@ bool mx4_operand_ok(uint64_t lines, uint64_t length, uint64_t batch, const void*
     return tiles <= 0x7fffffffull && (tiles == 0 || batch <= 0x7fffffffull / tiles);
 }
 
+// cuTensorMapEncodeTiled, by way of the runtime: the library is not linked against the driver.
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void* at = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &at, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+            at = nullptr;
+        return reinterpret_cast<EncodeTiled>(at);
+    }();
+    return f;
+}
+
+// The codes of an operand as bytes by lines by matrices, in boxes of 128 bytes of 128 lines.  x of a box is a multiple of 128 bytes; a line's pitch is a
+// multiple of 16.
+bool mx4_map(CUtensorMap* map, const uint8_t* codes, const MxOperand& op, uint64_t batch) {
+    const cuuint64_t pitch = (cuuint64_t)op.blocks * 16, dims[3] = {pitch, op.lines, batch}, strides[2] = {pitch, pitch * op.lines};
+    const cuuint32_t box[3] = {128, kMxTile, 1}, each[3] = {1, 1, 1};
+    const EncodeTiled encode = encode_tiled();
+    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(codes), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 } // namespace
 extern "C" {
 
@@ -1240,6 +1265,28 @@ int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, vo
                             ld, batch_stride, batch, op, codes_dev, scales_dev);
     };
     CUDA_TRY(dtype == KIMAD_F32 ? launch(static_cast<float*>(x_dev)) : launch(static_cast<__nv_bfloat16*>(x_dev)));
+    CUDA_TRY(cudaGetLastError());
+    return KIMAD_OK;
+}
+
+int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64_t m, uint64_t n, uint64_t length, uint64_t batch, const uint8_t* a_codes_dev,
+                      const uint8_t* a_scales_dev, const uint8_t* b_codes_dev, const uint8_t* b_scales_dev, float alpha, float beta, int32_t* status_dev,
+                      void* cuda_stream) {
+    if (ld < n || (uintptr_t)out_dev % 4 || (uintptr_t)status_dev % 4 || !mx4_operand_ok(m, length, batch, a_codes_dev, a_scales_dev) ||
+        !mx4_operand_ok(n, length, batch, b_codes_dev, b_scales_dev))
+        return KIMAD_ERR_INVALID_ARG;
+    if (m == 0 || n == 0 || batch == 0) return KIMAD_OK;
+    if (!out_dev || (length && (!a_codes_dev || !a_scales_dev || !b_codes_dev || !b_scales_dev)) || (batch > 1 && batch_stride < (m - 1) * ld + n))
+        return KIMAD_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const MxProduct p{out_dev, ld, batch_stride, a_scales_dev, b_scales_dev, MxOperand((uint32_t)m, (uint32_t)length), MxOperand((uint32_t)n, (uint32_t)length),
+                      alpha, beta, status_dev};
+    const uint64_t tiles = (uint64_t)p.a.line_tiles * p.b.line_tiles;
+    if (tiles > 0x7fffffffull || batch > 0x7fffffffull / tiles) return KIMAD_ERR_INVALID_ARG;
+    CUtensorMap map_a{}, map_b{}; // (not looked at where nothing is summed)
+    if (length && (!mx4_map(&map_a, a_codes_dev, p.a, batch) || !mx4_map(&map_b, b_codes_dev, p.b, batch))) return KIMAD_ERR_CUDA;
+    CUDA_TRY(cudaFuncSetAttribute(k_mx4_product, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxProductSmem));
+    CUDA_TRY(launch_pdl(k_mx4_product, dim3((uint32_t)(tiles * batch)), kMxProductThreads, kMxProductSmem, s, map_a, map_b, p));
     CUDA_TRY(cudaGetLastError());
     return KIMAD_OK;
 }

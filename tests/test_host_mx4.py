@@ -154,3 +154,35 @@ def test_binding_refuses_shapes_types_and_places():
         kb.kimad_mx4_dequantize(op, torch.zeros(3, 5, 7).half(), 0)
     with pytest.raises(ValueError):
         kb.Mx4Operand(7, 5, codes=torch.zeros(6, dtype=torch.uint8), scales=torch.zeros(512, dtype=torch.uint8))
+
+
+def test_product_refusals():
+    L = kb.load()
+    # out, ld, batch_stride, m, n, length, batch, a codes, a scales, b codes, b scales, alpha, beta, status, stream
+    good = [256, 7, 0, 5, 7, 40, 1, 512, 1024, 2048, 4096, C.c_float(1), C.c_float(0), None, None]
+    for i, v in [(0, None), (0, 258), (1, 6), (3, (1 << 30) + 1), (4, (1 << 30) + 1), (5, (1 << 30) + 1), (6, 2), (7, None), (7, 520), (8, None), (8, 1032), (9, None),
+                 (9, 2056), (10, None), (10, 4104), (13, 6)]:
+        a = list(good)
+        a[i] = v
+        assert L.kimad_mx4_product(*a) == BAD, (i, v)
+    for i in (3, 4, 6):  # nothing to do
+        a = list(good)
+        a[i] = 0
+        assert L.kimad_mx4_product(*a) == kb.KIMAD_OK
+    huge = list(good)
+    huge[3], huge[4], huge[1], huge[5] = 1 << 24, 1 << 24, 1 << 24, 1  # 2^34 tiles of outputs
+    assert L.kimad_mx4_product(*huge) == BAD
+
+
+def test_binding_refuses_products_of_what_does_not_fit():
+    import torch
+
+    def op(lines, length, batch=1):
+        return kb.Mx4Operand(lines, length, batch, device="cpu")
+
+    for a, b, out in [(op(5, 40), op(7, 41), torch.zeros(5, 7)), (op(5, 40, 2), op(7, 40), torch.zeros(2, 5, 7)), (op(5, 40), op(7, 40), torch.zeros(7, 5)),
+                      (op(5, 40), op(7, 40), torch.zeros(7, 5).t()), (op(5, 40), op(7, 40), torch.zeros(7).expand(5, 7)), (op(5, 40), op(7, 40), torch.zeros(5, 7))]:
+        with pytest.raises(ValueError):  # the last one: not on a CUDA device
+            kb.kimad_mx4_product(a, b, out)
+    with pytest.raises(TypeError):
+        kb.kimad_mx4_product(op(5, 40), op(7, 40), torch.zeros(5, 7, dtype=torch.bfloat16))
