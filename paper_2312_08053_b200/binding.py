@@ -427,25 +427,48 @@ def new_context(layer_sizes, n_workers, ratio_grid, device="cuda", **opts):
     return ctx
 
 
-def _mx4_dtype(t, what, names=("float32", "bfloat16", "float16")):
-    name = str(t.dtype).replace("torch.", "")
-    if name not in names:
-        raise TypeError(f"{what}: {name}, not one of {', '.join(names)}")
-    return {"float32": KIMAD_F32, "bfloat16": KIMAD_BF16, "float16": KIMAD_F16}[name]
+# The 4-bit calls are short (a few microseconds on the GPU for a small model), so what surrounds the C call is kept short too: types are looked up
+# by object, shapes compared as tuples, and the current stream asked for without making a Stream object of it.
+_MX4_DTYPES = {}
+_mx4_device = _mx4_raw_stream = None
 
 
-def _mx4_here(what, *tensors):
-    """The library takes memory of the current device (a tensor of another one is refused, as is one in host memory)."""
+def _mx4_setup():
+    global _mx4_device, _mx4_raw_stream
     import torch
 
+    _MX4_DTYPES.update({torch.float32: KIMAD_F32, torch.bfloat16: KIMAD_BF16, torch.float16: KIMAD_F16})
+    c = torch._C
+    _mx4_device = getattr(c, "_cuda_getDevice", torch.cuda.current_device)
+    _mx4_raw_stream = getattr(c, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _mx4_dtype(t, what, most=KIMAD_F16):
+    """The code of a tensor's type, one of float32, bfloat16, float16 up to `most`."""
+    if not _MX4_DTYPES:
+        _mx4_setup()
+    code = _MX4_DTYPES.get(t.dtype, 99)
+    if code > most:
+        raise TypeError(f"{what}: {t.dtype}, not one of {list(_MX4_DTYPES)[:most + 1]}")
+    return code
+
+
+def _mx4_stream(what, stream, *tensors):
+    """The library takes memory of the current device: a tensor of another one is refused, as is one in host memory."""
     for t in tensors:
-        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        if not t.is_cuda:
             raise ValueError(f"{what}: tensor on {t.device}, not on the current CUDA device")
+    device = _mx4_device()
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError(f"{what}: tensor on {t.device}, the current device is cuda:{device}")
+    return _mx4_raw_stream(device) if stream is None else _stream_ptr(stream)
 
 
 def _mx4_workers(ctx, t, what):
-    if t.dim() != 2 or t.shape[0] != ctx.W or t.shape[1] < ctx.N or (t.shape[1] > 1 and t.stride(1) != 1) or (ctx.W > 1 and t.stride(0) != ctx.stride):
-        raise ValueError(f"{what}: [{ctx.W}][{ctx.stride}] with rows of consecutive elements, not {tuple(t.shape)} with strides {t.stride()}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != ctx.W or shape[1] < ctx.N or (shape[1] > 1 and stride[1] != 1) or (ctx.W > 1 and stride[0] != ctx.stride):
+        raise ValueError(f"{what}: [{ctx.W}][{ctx.stride}] with rows of consecutive elements, not {tuple(shape)} with strides {stride}")
 
 
 def kimad_mx4_message_bytes(ctx: Ctx):
@@ -455,68 +478,74 @@ def kimad_mx4_message_bytes(ctx: Ctx):
     return int(c.value), int(s.value)
 
 
+def _mx4_shape(ctx):
+    """What two contexts share that can read each other's messages."""
+    shape = getattr(ctx, "_mx4_shape", None)
+    if shape is None:
+        shape = ctx._mx4_shape = (ctx.W, ctx.L, *kimad_mx4_message_bytes(ctx))
+    return shape
+
+
 class Mx4Message:
-    """Device buffers of all workers' 4-bit messages and the matching ``kimad_mx4_message`` struct."""
+    """Device buffers of all workers' 4-bit messages (tensors that stay where they are) and the matching ``kimad_mx4_message`` struct."""
 
     def __init__(self, ctx: Ctx, device="cuda"):
         import torch
 
-        code_bytes, scale_bytes = kimad_mx4_message_bytes(ctx)
-        self.codes = torch.zeros((ctx.W, code_bytes), dtype=torch.uint8, device=device)
-        self.scales = torch.zeros((ctx.W, scale_bytes), dtype=torch.uint8, device=device)
-        self.err = torch.zeros((ctx.W, ctx.L), dtype=torch.float32, device=device)
-        self.stats = torch.zeros((ctx.W, STATS_DTYPE.itemsize), dtype=torch.uint8, device=device)
+        self.shape = _mx4_shape(ctx)
+        W, L, code_bytes, scale_bytes = self.shape
+        self.codes = torch.zeros((W, code_bytes), dtype=torch.uint8, device=device)
+        self.scales = torch.zeros((W, scale_bytes), dtype=torch.uint8, device=device)
+        self.err = torch.zeros((W, L), dtype=torch.float32, device=device)
+        self.stats = torch.zeros((W, STATS_DTYPE.itemsize), dtype=torch.uint8, device=device)
         self.c = kimad_mx4_message(self.codes.data_ptr(), self.scales.data_ptr(), self.err.data_ptr(), self.stats.data_ptr())
+        self.ref = C.byref(self.c)
 
     def stats_host(self) -> np.ndarray:
         return self.stats.cpu().numpy().view(STATS_DTYPE).reshape(-1)
 
 
 def _mx4_message(ctx, msg, what):
-    """The struct of a message, whose buffers have to be those of a context of this shape."""
-    code_bytes, scale_bytes = kimad_mx4_message_bytes(ctx)
-    if tuple(msg.codes.shape) != (ctx.W, code_bytes) or tuple(msg.scales.shape) != (ctx.W, scale_bytes) or tuple(msg.err.shape) != (ctx.W, ctx.L):
+    if msg.shape != _mx4_shape(ctx):
         raise ValueError(f"{what}: a message of another context's shape")
-    _mx4_here(what, msg.codes)
-    return C.byref(msg.c)
+    return msg.ref
 
 
 def kimad_mx4_step(ctx: Ctx, grads, state, msg: Mx4Message, stream=None) -> None:
     """grads: CUDA float32, bfloat16 or float16 [W][ctx.stride]; state: CUDA float32 of that shape, updated in place."""
     dtype = _mx4_dtype(grads, "grads")
-    _mx4_dtype(state, "state", ("float32",))
-    for t, what in ((grads, "grads"), (state, "state")):
-        _mx4_workers(ctx, t, what)
+    _mx4_dtype(state, "state", KIMAD_F32)
+    _mx4_workers(ctx, grads, "grads")
+    _mx4_workers(ctx, state, "state")
     m = _mx4_message(ctx, msg, "kimad_mx4_step")
-    _mx4_here("kimad_mx4_step", grads, state)
-    _check(load().kimad_mx4_step(ctx.handle, grads.data_ptr(), dtype, state.data_ptr(), m, _stream_ptr(stream)), "kimad_mx4_step")
+    s = _mx4_stream("kimad_mx4_step", stream, grads, state, msg.codes)
+    _check(load().kimad_mx4_step(ctx.handle, grads.data_ptr(), dtype, state.data_ptr(), m, s), "kimad_mx4_step")
 
 
 def kimad_mx4_apply(ctx: Ctx, msg: Mx4Message, est, x=None, weights=None, gamma=0.0, stream=None) -> None:
     """est: CUDA float32 [W][ctx.stride], in place.  With x (CUDA float32 [N], in place) also the model step: weights, W host floats, and gamma."""
-    _mx4_dtype(est, "est", ("float32",))
+    _mx4_dtype(est, "est", KIMAD_F32)
     _mx4_workers(ctx, est, "est")
     m = _mx4_message(ctx, msg, "kimad_mx4_apply")
-    _mx4_here("kimad_mx4_apply", est)
     if x is None:
-        _check(load().kimad_mx4_apply(ctx.handle, m, est.data_ptr(), None, None, C.c_float(0.0), _stream_ptr(stream)), "kimad_mx4_apply")
+        s = _mx4_stream("kimad_mx4_apply", stream, est, msg.codes)
+        _check(load().kimad_mx4_apply(ctx.handle, m, est.data_ptr(), None, None, 0.0, s), "kimad_mx4_apply")
         return
-    _mx4_dtype(x, "x", ("float32",))
+    _mx4_dtype(x, "x", KIMAD_F32)
     w = np.ascontiguousarray([] if weights is None else weights, dtype=np.float32).reshape(-1)
     if w.size != ctx.W or x.dim() != 1 or x.numel() != ctx.N or (ctx.N > 1 and x.stride(0) != 1):
         raise ValueError(f"kimad_mx4_apply: x of {ctx.N} consecutive elements and {ctx.W} weights")
-    _mx4_here("kimad_mx4_apply", x)
-    _check(load().kimad_mx4_apply(ctx.handle, m, est.data_ptr(), x.data_ptr(), w.ctypes.data_as(C.POINTER(C.c_float)), C.c_float(gamma),
-                                  _stream_ptr(stream)), "kimad_mx4_apply")
+    s = _mx4_stream("kimad_mx4_apply", stream, est, x, msg.codes)
+    _check(load().kimad_mx4_apply(ctx.handle, m, est.data_ptr(), x.data_ptr(), w.ctypes.data_as(C.POINTER(C.c_float)), gamma, s), "kimad_mx4_apply")
 
 
 def kimad_mx4_read(ctx: Ctx, msg: Mx4Message, out, stream=None) -> None:
     """out: CUDA float32 or bfloat16 [W][ctx.stride], the values that the messages stand for."""
-    dtype = _mx4_dtype(out, "out", ("float32", "bfloat16"))
+    dtype = _mx4_dtype(out, "out", KIMAD_BF16)
     _mx4_workers(ctx, out, "out")
     m = _mx4_message(ctx, msg, "kimad_mx4_read")
-    _mx4_here("kimad_mx4_read", out)
-    _check(load().kimad_mx4_read(ctx.handle, m, out.data_ptr(), dtype, _stream_ptr(stream)), "kimad_mx4_read")
+    s = _mx4_stream("kimad_mx4_read", stream, out, msg.codes)
+    _check(load().kimad_mx4_read(ctx.handle, m, out.data_ptr(), dtype, s), "kimad_mx4_read")
 
 
 def kimad_mx4_operand_bytes(lines: int, length: int):
@@ -542,60 +571,60 @@ class Mx4Operand:
                 raise ValueError(f"an operand of {batch} x {lines} x {length} has {batch * n} contiguous bytes, not {tuple(t.shape)} of {t.dtype}")
 
 
-def _mx4_matrix(t, op, along, what):
-    """(batch, rows, cols, row stride, matrix stride) of a [rows][cols] or [batch][rows][cols] tensor that goes with an operand."""
-    if t.dim() == 2:
-        t = t[None]
-    if t.dim() != 3 or along not in (0, 1):
-        raise ValueError(f"{what}: [rows][cols] or [batch][rows][cols], along 0 or 1")
-    b, rows, cols = t.shape
-    if (b, rows, cols) != (op.batch, *((op.length, op.lines) if along == 0 else (op.lines, op.length))):
-        raise ValueError(f"{what}: {tuple(t.shape)} along {along} is not an operand of {op.batch} x {op.lines} x {op.length}")
-    if cols > 1 and t.stride(2) != 1:
-        raise ValueError(f"{what}: columns have to be consecutive elements, not {t.stride(2)} apart")
-    ld = t.stride(1) if rows > 1 else cols
-    if ld < cols:
-        raise ValueError(f"{what}: rows overlap")
-    return b, rows, cols, ld, t.stride(0) if b > 1 else 0
+def _mx4_matrix(t, batch, rows, cols, what):
+    """(row stride, matrix stride) of a [rows][cols] or [batch][rows][cols] tensor."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        shape, stride = (1, *shape), (0, *stride)
+    if tuple(shape) != (batch, rows, cols):
+        raise ValueError(f"{what}: {tuple(t.shape)} does not go with an operand, {batch} x {rows} x {cols} does")
+    ld = stride[1] if rows > 1 else cols
+    if (cols > 1 and stride[2] != 1) or ld < cols:
+        raise ValueError(f"{what}: rows of consecutive elements that do not overlap, not strides {t.stride()}")
+    return ld, stride[0] if batch > 1 else 0
+
+
+def _mx4_along(op, along):
+    if along not in (0, 1):
+        raise ValueError("along: 0, blocks over the rows, or 1, over the columns")
+    return (op.length, op.lines) if along == 0 else (op.lines, op.length)
 
 
 def kimad_mx4_quantize(x, op: Mx4Operand, along: int, stream=None) -> None:
     """x: CUDA float32, bfloat16 or float16, [rows][cols] or [batch][rows][cols].  along 0: blocks over the rows (the operand is x transposed), 1: over
     the columns."""
     dtype = _mx4_dtype(x, "x")
-    b, rows, cols, ld, bs = _mx4_matrix(x, op, along, "x")
-    _mx4_here("kimad_mx4_quantize", x, op.codes, op.scales)
-    _check(load().kimad_mx4_quantize(x.data_ptr(), dtype, rows, cols, ld, b, bs, along, op.codes.data_ptr(), op.scales.data_ptr(), _stream_ptr(stream)),
+    rows, cols = _mx4_along(op, along)
+    ld, bs = _mx4_matrix(x, op.batch, rows, cols, "x")
+    s = _mx4_stream("kimad_mx4_quantize", stream, x, op.codes, op.scales)
+    _check(load().kimad_mx4_quantize(x.data_ptr(), dtype, rows, cols, ld, op.batch, bs, along, op.codes.data_ptr(), op.scales.data_ptr(), s),
            "kimad_mx4_quantize")
 
 
 def kimad_mx4_dequantize(op: Mx4Operand, out, along: int, stream=None) -> None:
     """out: CUDA float32 or bfloat16, shaped as kimad_mx4_quantize's x."""
-    dtype = _mx4_dtype(out, "out", ("float32", "bfloat16"))
-    b, rows, cols, ld, bs = _mx4_matrix(out, op, along, "out")
-    _mx4_here("kimad_mx4_dequantize", out, op.codes, op.scales)
-    _check(load().kimad_mx4_dequantize(op.codes.data_ptr(), op.scales.data_ptr(), out.data_ptr(), dtype, rows, cols, ld, b, bs, along, _stream_ptr(stream)),
+    dtype = _mx4_dtype(out, "out", KIMAD_BF16)
+    rows, cols = _mx4_along(op, along)
+    ld, bs = _mx4_matrix(out, op.batch, rows, cols, "out")
+    s = _mx4_stream("kimad_mx4_dequantize", stream, out, op.codes, op.scales)
+    _check(load().kimad_mx4_dequantize(op.codes.data_ptr(), op.scales.data_ptr(), out.data_ptr(), dtype, rows, cols, ld, op.batch, bs, along, s),
            "kimad_mx4_dequantize")
 
 
 def kimad_mx4_product(a: Mx4Operand, b: Mx4Operand, out, alpha=1.0, beta=0.0, status=None, stream=None) -> None:
     """out <- beta out + alpha a b^T.  out: CUDA float32 [a.lines][b.lines] or [batch][a.lines][b.lines], rows of consecutive elements at any stride
     and place; status: CUDA int32 tensor of one element or None."""
-    _mx4_dtype(out, "out", ("float32",))
-    if (a.length, a.batch) != (b.length, b.batch):
+    _mx4_dtype(out, "out", KIMAD_F32)
+    if a.length != b.length or a.batch != b.batch:
         raise ValueError(f"kimad_mx4_product: operands of {a.batch} x {a.length} and of {b.batch} x {b.length}")
-    o = out[None] if out.dim() == 2 else out
-    if tuple(o.shape) != (a.batch, a.lines, b.lines) or (b.lines > 1 and o.stride(2) != 1):
-        raise ValueError(f"kimad_mx4_product: out of {a.batch} x {a.lines} x {b.lines} with rows of consecutive elements, not {tuple(out.shape)}")
-    ld = o.stride(1) if a.lines > 1 else b.lines
-    if ld < b.lines:
-        raise ValueError("kimad_mx4_product: rows of out overlap")
-    _mx4_here("kimad_mx4_product", out, a.codes, a.scales, b.codes, b.scales, *(() if status is None else (status,)))
-    if status is not None and (str(status.dtype) != "torch.int32" or status.numel() < 1):
-        raise TypeError("kimad_mx4_product: status is an int32 tensor")
-    _check(load().kimad_mx4_product(out.data_ptr(), ld, o.stride(0) if a.batch > 1 else 0, a.lines, b.lines, a.length, a.batch, a.codes.data_ptr(),
-                                    a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), C.c_float(alpha), C.c_float(beta),
-                                    None if status is None else status.data_ptr(), _stream_ptr(stream)), "kimad_mx4_product")
+    ld, bs = _mx4_matrix(out, a.batch, a.lines, b.lines, "out")
+    s = _mx4_stream("kimad_mx4_product", stream, out, a.codes, a.scales, b.codes, b.scales)
+    if status is not None:
+        if str(status.dtype) != "torch.int32" or status.numel() < 1:
+            raise TypeError("kimad_mx4_product: status is an int32 tensor")
+        _mx4_stream("kimad_mx4_product", stream, status)
+    _check(load().kimad_mx4_product(out.data_ptr(), ld, bs, a.lines, b.lines, a.length, a.batch, a.codes.data_ptr(), a.scales.data_ptr(),
+                                    b.codes.data_ptr(), b.scales.data_ptr(), alpha, beta, None if status is None else status.data_ptr(), s), "kimad_mx4_product")
 
 
 class Monitor:

@@ -2,6 +2,7 @@
 // chunk table, workspace layout) and the per-step launch sequence.  No device memory is allocated
 // here; the caller's workspace is carved into the regions listed in `Layout`.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdlib>
 #include <cstdio>
@@ -1136,6 +1137,19 @@ EncodeTiled encode_tiled() {
     return f;
 }
 
+// The product's shared memory is above the default limit, which is raised once on every device.
+int mx4_prepare_product() {
+    static std::atomic<uint64_t> raised[4] = {};
+    int dev = 0;
+    CUDA_TRY(cudaGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev >= 256 || !(raised[dev / 64].load(std::memory_order_acquire) & bit)) {
+        CUDA_TRY(cudaFuncSetAttribute(k_mx4_product, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxProductSmem));
+        if (dev < 256) raised[dev / 64].fetch_or(bit, std::memory_order_release);
+    }
+    return KIMAD_OK;
+}
+
 // The codes of an operand as bytes by lines by matrices, in boxes of 128 bytes of 128 lines.  x of a box is a multiple of 128 bytes; a line's pitch is a
 // multiple of 16.
 bool mx4_map(CUtensorMap* map, const uint8_t* codes, const MxOperand& op, uint64_t batch) {
@@ -1285,7 +1299,7 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
     if (tiles > 0x7fffffffull || batch > 0x7fffffffull / tiles) return KIMAD_ERR_INVALID_ARG;
     CUtensorMap map_a{}, map_b{}; // (not looked at where nothing is summed)
     if (length && (!mx4_map(&map_a, a_codes_dev, p.a, batch) || !mx4_map(&map_b, b_codes_dev, p.b, batch))) return KIMAD_ERR_CUDA;
-    CUDA_TRY(cudaFuncSetAttribute(k_mx4_product, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxProductSmem));
+    { const int rc = mx4_prepare_product(); if (rc != KIMAD_OK) return rc; }
     CUDA_TRY(launch_pdl(k_mx4_product, dim3((uint32_t)(tiles * batch)), kMxProductThreads, kMxProductSmem, s, map_a, map_b, p));
     CUDA_TRY(cudaGetLastError());
     return KIMAD_OK;
