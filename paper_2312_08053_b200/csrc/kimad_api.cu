@@ -1114,6 +1114,8 @@ bool mx4_message_ok(const kimad_ctx* c, const kimad_mx4_message* m) {
            c->W <= 65535;
 }
 
+MxMessage mx4_buffers(const kimad_ctx* c, const kimad_mx4_message* m) { return MxMessage{m->codes, m->scales, mx4_code_bytes(c), mx4_scale_bytes(c)}; }
+
 // What the calls on matrices check: 0 < lines, length <= 2^30, buffers on 16 bytes, tiles within a grid.
 constexpr uint64_t kMxMostLines = 1ull << 30;
 bool mx4_operand_ok(uint64_t lines, uint64_t length, uint64_t batch, const void* codes, const void* scales) {
@@ -1181,8 +1183,7 @@ int kimad_mx4_step(kimad_ctx* c, const void* grads_dev, uint32_t grad_dtype, flo
     const LayerDesc* layers = c->at<LayerDesc>(c->lay.layers);
     MxPartial* partial = c->at<MxPartial>(c->lay.csel); // (the selection of a TopK step is over when this runs, and starts from its own counts)
     auto launch = [&](auto kern, auto* grads) {
-        return launch_named("k_mx4_step", kern, dim3(nch << lp, c->W), kThreads, 0, s, grads, state_dev, c->stride, chunks, layers, lp, out->codes,
-                            out->scales, mx4_code_bytes(c), mx4_scale_bytes(c), partial);
+        return launch_named("k_mx4_step", kern, dim3(nch << lp, c->W), kThreads, 0, s, grads, state_dev, c->stride, chunks, layers, lp, mx4_buffers(c, out), partial);
     };
     CUDA_TRY(grad_dtype == KIMAD_F32 ? launch(k_mx4_step<float>, static_cast<const float*>(grads_dev))
              : grad_dtype == KIMAD_BF16 ? launch(k_mx4_step<__nv_bfloat16>, static_cast<const __nv_bfloat16*>(grads_dev))
@@ -1203,8 +1204,7 @@ int kimad_mx4_apply(const kimad_ctx* c, const kimad_mx4_message* msg, float* est
     MxWeights wt{};
     for (uint32_t m = 0; x_dev && m < c->W; ++m) wt.w[m] = weights[m];
     auto launch = [&](auto kern) {
-        return launch_named("k_mx4_apply", kern, dim3(nch << lp, rows), kThreads, 0, s, msg->codes, msg->scales, mx4_code_bytes(c), mx4_scale_bytes(c),
-                            c->at<const Chunk>(c->lay.chunks), c->at<const LayerDesc>(c->lay.layers), lp, est_dev, c->stride, c->W, x_dev, wt, gamma);
+        return launch_named("k_mx4_apply", kern, dim3(nch << lp, rows), kThreads, 0, s, mx4_buffers(c, msg), c->at<const Chunk>(c->lay.chunks), c->at<const LayerDesc>(c->lay.layers), lp, est_dev, c->stride, c->W, x_dev, wt, gamma);
     };
     CUDA_TRY(x_dev ? launch(k_mx4_apply<true>) : launch(k_mx4_apply<false>));
     CUDA_TRY(cudaGetLastError());
@@ -1217,8 +1217,7 @@ int kimad_mx4_read(const kimad_ctx* c, const kimad_mx4_message* msg, void* out_d
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const uint32_t nch = (uint32_t)c->chunks.size(), lp = mx4_log_pieces((uint64_t)nch * c->W);
     auto launch = [&](auto kern, auto* out) {
-        return launch_named("k_mx4_read", kern, dim3(nch << lp, c->W), kThreads, 0, s, msg->codes, msg->scales, mx4_code_bytes(c), mx4_scale_bytes(c),
-                            c->at<const Chunk>(c->lay.chunks), c->at<const LayerDesc>(c->lay.layers), lp, out, c->stride);
+        return launch_named("k_mx4_read", kern, dim3(nch << lp, c->W), kThreads, 0, s, mx4_buffers(c, msg), c->at<const Chunk>(c->lay.chunks), c->at<const LayerDesc>(c->lay.layers), lp, out, c->stride);
     };
     CUDA_TRY(dtype == KIMAD_F32 ? launch(k_mx4_read<float>, static_cast<float*>(out_dev))
                                 : launch(k_mx4_read<__nv_bfloat16>, static_cast<__nv_bfloat16*>(out_dev)));
@@ -1247,10 +1246,9 @@ int kimad_mx4_quantize(const void* x_dev, uint32_t dtype, uint64_t rows, uint64_
     auto launch = [&](auto* x) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(x)>>;
         if (along == 0)
-            return launch_named("k_mx4_quantize_cols", k_mx4_quantize_cols<T>, dim3((uint32_t)(batch * op.line_tiles * op.block_tiles)), kMxColThreads, 0, s, x,
+            return launch_named("k_mx4_quantize_cols", k_mx4_quantize_cols<T>, dim3((uint32_t)(batch * op.line_tiles * op.block_tiles)), kThreads, 0, s, x,
                                 ld, batch_stride, op, codes_dev, scales_dev);
-        const uint64_t warps = batch * op.line_tiles * kMxTile * ((op.blocks + kMxGroup - 1) / kMxGroup);
-        return launch_named("k_mx4_quantize_rows", k_mx4_quantize_rows<T>, dim3((uint32_t)std::min<uint64_t>((warps + 7) / 8, 148 * 32)), kThreads, 0, s, x,
+        return launch_named("k_mx4_quantize_rows", k_mx4_quantize_rows<T>, dim3((uint32_t)std::min<uint64_t>(batch * MxRowCuts(op).ctas(), 1u << 30)), kThreads, 0, s, x,
                             ld, batch_stride, batch, op, codes_dev, scales_dev);
     };
     CUDA_TRY(dtype == KIMAD_F32 ? launch(static_cast<const float*>(x_dev))
@@ -1272,10 +1270,9 @@ int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, vo
     auto launch = [&](auto* x) {
         using T = std::remove_pointer_t<decltype(x)>;
         if (along == 0)
-            return launch_named("k_mx4_dequantize_cols", k_mx4_dequantize_cols<T>, dim3((uint32_t)(batch * op.line_tiles * op.block_tiles)), kMxColThreads, 0, s, x,
+            return launch_named("k_mx4_dequantize_cols", k_mx4_dequantize_cols<T>, dim3((uint32_t)(batch * op.line_tiles * op.block_tiles)), kThreads, 0, s, x,
                                 ld, batch_stride, op, codes_dev, scales_dev);
-        const uint64_t warps = batch * op.lines * ((op.blocks + kMxGroup - 1) / kMxGroup);
-        return launch_named("k_mx4_dequantize_rows", k_mx4_dequantize_rows<T>, dim3((uint32_t)std::min<uint64_t>((warps + 7) / 8, 148 * 32)), kThreads, 0, s, x,
+        return launch_named("k_mx4_dequantize_rows", k_mx4_dequantize_rows<T>, dim3((uint32_t)std::min<uint64_t>(batch * MxRowCuts(op).ctas(), 1u << 30)), kThreads, 0, s, x,
                             ld, batch_stride, batch, op, codes_dev, scales_dev);
     };
     CUDA_TRY(dtype == KIMAD_F32 ? launch(static_cast<float*>(x_dev)) : launch(static_cast<__nv_bfloat16*>(x_dev)));
