@@ -1147,16 +1147,17 @@ int mx4_prepare_product() {
     const uint64_t bit = 1ull << (dev & 63);
     if (dev >= 256 || !(raised[dev / 64].load(std::memory_order_acquire) & bit)) {
         CUDA_TRY(cudaFuncSetAttribute(k_mx4_product, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxProductSmem));
+        CUDA_TRY(cudaFuncSetAttribute(k_mx4_product_pairs, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxPairSmem));
         if (dev < 256) raised[dev / 64].fetch_or(bit, std::memory_order_release);
     }
     return KIMAD_OK;
 }
 
-// The codes of an operand as bytes by lines by matrices, in boxes of 128 bytes of 128 lines.  x of a box is a multiple of 128 bytes; a line's pitch is a
+// The codes of an operand as bytes by lines by matrices, in boxes of 128 bytes of some lines.  x of a box is a multiple of 128 bytes; a line's pitch is a
 // multiple of 16.
-bool mx4_map(CUtensorMap* map, const uint8_t* codes, const MxOperand& op, uint64_t batch) {
+bool mx4_map(CUtensorMap* map, const uint8_t* codes, const MxOperand& op, uint64_t batch, uint32_t box_lines) {
     const cuuint64_t pitch = (cuuint64_t)op.blocks * 16, dims[3] = {pitch, op.lines, batch}, strides[2] = {pitch, pitch * op.lines};
-    const cuuint32_t box[3] = {128, kMxTile, 1}, each[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {128, box_lines, 1}, each[3] = {1, 1, 1};
     const EncodeTiled encode = encode_tiled();
     return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(codes), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -1294,9 +1295,18 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
                       alpha, beta, status_dev};
     const uint64_t tiles = (uint64_t)p.a.line_tiles * p.b.line_tiles;
     if (tiles > 0x7fffffffull || batch > 0x7fffffffull / tiles) return KIMAD_ERR_INVALID_ARG;
+    const uint64_t pair_tiles = (m + 255) / 256 * ((n + kMxPairN - 1) / kMxPairN) * batch;
+    const bool pairs = length && pair_tiles >= 74;
     CUtensorMap map_a{}, map_b{}; // (not looked at where nothing is summed)
-    if (length && (!mx4_map(&map_a, a_codes_dev, p.a, batch) || !mx4_map(&map_b, b_codes_dev, p.b, batch))) return KIMAD_ERR_CUDA;
+    if (length && (!mx4_map(&map_a, a_codes_dev, p.a, batch, kMxTile) || !mx4_map(&map_b, b_codes_dev, p.b, batch, pairs ? kMxPairN / 2 : kMxTile)))
+        return KIMAD_ERR_CUDA;
     { const int rc = mx4_prepare_product(); if (rc != KIMAD_OK) return rc; }
+    if (pairs) {
+        CUDA_TRY(launch_pdl(k_mx4_product_pairs, dim3((uint32_t)std::min<uint64_t>(pair_tiles, 74) * 2), kMxPairThreads, kMxPairSmem, s, map_a, map_b, p,
+                            (uint32_t)pair_tiles));
+        CUDA_TRY(cudaGetLastError());
+        return KIMAD_OK;
+    }
     CUDA_TRY(launch_pdl(k_mx4_product, dim3((uint32_t)(tiles * batch)), kMxProductThreads, kMxProductSmem, s, map_a, map_b, p));
     CUDA_TRY(cudaGetLastError());
     return KIMAD_OK;

@@ -2,12 +2,15 @@
 //
 // tcgen05.mma of kind mxf4 takes the codes as they lie in the operands (K-major, two to a byte), 64 values of the summed axis at a time, and
 // the two scales a line that go with them; products of codes are exact, scaled by powers of two and added in binary32 in tensor memory.  The
-// scales' tiles (128 lines by 4 blocks, 512 bytes) are in the order that tensor memory wants: lane r % 32, column r / 32, a byte per block.
+// scales' tiles (128 lines by 4 blocks, 512 bytes) are in the order that tensor memory wants: lane r % 32 (in all four quarters of it), column
+// r / 32, a byte per block.
 //
 // A CTA makes a tile of 128 by 128 outputs: one warp brings stages of 256 values (128 bytes) of 128 lines of either operand by TMA, 128-byte
-// swizzled, and their scales by bulk copies; one thread of another warp copies the scales to tensor memory and issues the products; four warps
-// take the sums out (32 lines each), turn slabs of 32 by 32 around in shared memory and update the output in lines of consecutive elements,
-// whatever its alignment.  Two CTAs share an SM: one's outputs are written beside the other's products.
+// swizzled, and their scales by bulk copies; four warps store the scales to tensor memory, a quarter each; one thread of another warp issues the
+// products.  (Copies of the scales by tcgen05.cp wait in line with the products: a stage then took 590 clocks of an SM, 256 of them products.)
+// The four warps then take the sums out (32 lines each), turn slabs of 32 by 32 around in shared memory and update the output in lines of
+// consecutive elements, whatever its alignment; the first of the output's old values are under way while the products run.  Two CTAs share
+// an SM: one's outputs are written beside the other's products.
 // Lines behind the operand's last and bytes behind a line's last block are filled with zeros by TMA: code 0 times any scale that is there
 // is 0, and the scales that are not there are 0 too.
 // Waits are bounded (kMxWaitClocks): a CTA whose wait ran out stores nothing, waits for its copies, frees its tensor memory and sets the status.
@@ -21,26 +24,22 @@ namespace kimad {
 constexpr int kMxStages = 3;
 constexpr uint32_t kMxStageK = 256;                  // values of the summed axis in a stage
 constexpr uint32_t kMxOperandStage = 128 * 128;      // bytes of codes of an operand in a stage
-constexpr uint32_t kMxScaleStage = 2 * 512;          // ... and of scales
-constexpr uint32_t kMxStageBytes = 2 * kMxOperandStage + 2 * kMxScaleStage;
+constexpr uint32_t kMxStageBytes = 2 * kMxOperandStage;
 constexpr uint32_t kMxProductSmem = 1024 + kMxStages * kMxStageBytes;
-constexpr int kMxProductThreads = 192;               // warps 0-3 outputs, 4 copies, 5 products
+constexpr int kMxProductThreads = 192;               // warps 0-3 scales and outputs, 4 copies, 5 products
 constexpr uint32_t kMxTmemCols = 256;                // 128 of sums, 16 of scales a stage
 constexpr long long kMxWaitClocks = 1ll << 31;       // about a second
 
-// Instruction descriptor of kind mxf4: E2M1 by E2M1, scales UE8M0, K-major, N = 128 (bits 17-22, in eights), M = 128 (bits 27-28, in 128s).
+// Instruction descriptor of kind mxf4: E2M1 by E2M1, scales UE8M0, K-major, N (bits 17-22, in eights), M (bits 27-28, in 128s).
 // The two scales of a product lie in bytes 0-1 or 2-3 of their column (bits 4-5 for B, 29-30 for A).
-constexpr uint32_t kMxIdesc = (1u << 7) | (1u << 10) | ((128u / 8u) << 17) | (1u << 23) | (1u << 27);
-__device__ __forceinline__ uint32_t mx_idesc(uint32_t half) { return kMxIdesc | (half * 2u) << 4 | (half * 2u) << 29; }
+KIMAD_HD constexpr uint32_t mx_idesc(uint32_t m, uint32_t n, uint32_t half) {
+    return (1u << 7) | (1u << 10) | ((n / 8u) << 17) | (1u << 23) | ((m / 128u) << 27) | (half * 2u) << 4 | (half * 2u) << 29;
+}
 
-// Shared-memory descriptors: lines of 128 bytes, 128-byte swizzle, eight lines to 1024 bytes; and for the scales no swizzle, eight rows of 16 bytes to 128.
+// Shared-memory descriptor: lines of 128 bytes, 128-byte swizzle, eight lines to 1024 bytes.
 __device__ __forceinline__ uint64_t mx_desc_codes(uint32_t addr) {
     return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-__device__ __forceinline__ uint64_t mx_desc_scales(uint32_t addr) {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(128 >> 4) << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
-}
-
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -58,23 +57,34 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
         if (*failed || clock64() - began > kMxWaitClocks) { *failed = 1; return false; }
     return true;
 }
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x),
                  "r"(y), "r"(z), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void tc_store16(uint32_t addr, const uint4 (&v)[4]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(v[0].x), "r"(v[0].y),
+                 "r"(v[0].z), "r"(v[0].w), "r"(v[1].x), "r"(v[1].y), "r"(v[1].z), "r"(v[1].w), "r"(v[2].x), "r"(v[2].y), "r"(v[2].z), "r"(v[2].w), "r"(v[3].x),
+                 "r"(v[3].y), "r"(v[3].z), "r"(v[3].w) : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// GROUP: CTAs whose tensor cores take one product together.
+template <int GROUP> __device__ __forceinline__ void tc_mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    if (GROUP == 1)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
+                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa),
+                     "r"(sb), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
+                     "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa),
+                     "r"(sb), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-}
-__device__ __forceinline__ void tc_mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
-                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa),
-                 "r"(sb), "r"(accumulate) : "memory");
+// Arrival when all products issued so far are done: on this CTA's barrier, or on both CTAs' of a pair.
+template <int GROUP> __device__ __forceinline__ void tc_commit(uint32_t bar) {
+    if (GROUP == 1) asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
 }
 __device__ __forceinline__ void tc_load32(uint32_t (&r)[32], uint32_t addr) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -85,6 +95,23 @@ __device__ __forceinline__ void tc_load32(uint32_t (&r)[32], uint32_t addr) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// One lane of a warp, the same one every time.  (With a lane's number in its place, and roles by a thread's number, the compiler does not see that addresses
+// and descriptors are the same for the whole warp, and every copy and product takes about 100 clocks to issue.)
+__device__ __forceinline__ bool one_lane() {
+    uint32_t one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
+__device__ __forceinline__ uint32_t warp_number() { return __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0); }
+
+// A place in a ring of barriers and the parity of its present phase.
+template <uint32_t N> struct MxRing {
+    uint32_t s = 0, parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == N) { s = 0; parity ^= 1u; }
+    }
+};
+
 struct MxProduct {
     float* out;
     uint64_t ld, batch_stride;
@@ -94,20 +121,87 @@ struct MxProduct {
     int32_t* status;
 };
 
-__global__ void __launch_bounds__(kMxProductThreads)
+// A warp's part of the output, 32 rows by slabs of 32 columns.  A lane has a row of the sums, as tensor memory gives them.  Where the output's rows lie on
+// 32 bytes and a slab is whole, a lane updates its row by four accesses of 32 bytes (whole sectors), whose old values can be fetched ahead; elsewhere the slab
+// is turned around in shared memory (`buf`, 32 x 33) and updated in lines of consecutive elements, any alignment and any edge.
+struct MxOutput {
+    float* at;   // row 0, column 0
+    float* mine; // this lane's row
+    uint64_t ld;
+    uint32_t rows, cols; // that are there
+    float alpha, beta;
+    uint32_t lane;
+    bool aligned;
+    __device__ __forceinline__ MxOutput(const MxProduct& p, uint32_t n, uint32_t row, uint32_t col, uint32_t most_cols, uint32_t lane_)
+        : at(p.out + n * p.batch_stride + (uint64_t)row * p.ld + col), ld(p.ld), alpha(p.alpha), beta(p.beta), lane(lane_) {
+        mine = at + lane * ld;
+        rows = row < p.a.lines ? min(p.a.lines - row, 32u) : 0u;
+        cols = col < p.b.lines ? min(p.b.lines - col, most_cols) : 0u;
+        aligned = reinterpret_cast<uintptr_t>(at) % 32 == 0 && ld % 8 == 0;
+    }
+    __device__ __forceinline__ bool whole(uint32_t slab) const { return aligned && 32 * slab + 32 <= cols; }
+    __device__ __forceinline__ void fetch(uint32_t slab, float (&was)[32]) const {
+        if (beta != 0.f && whole(slab) && lane < rows) {
+#pragma unroll
+            for (uint32_t i = 0; i < 32; i += 8) mx_load8(mine + 32 * slab + i, *reinterpret_cast<float(*)[8]>(&was[i]));
+        }
+    }
+    __device__ __forceinline__ float update(uint32_t sum, float was) const {
+        const float x = __fmul_rn(alpha, __uint_as_float(sum));
+        return beta != 0.f ? __fmaf_rn(beta, was, x) : x;
+    }
+    __device__ __forceinline__ void put(uint32_t slab, const uint32_t (&sums)[32], const float (&was)[32], float* buf) const {
+        if (whole(slab)) {
+            if (lane < rows) {
+#pragma unroll
+                for (uint32_t i = 0; i < 32; i += 8) {
+                    float x[8];
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) x[j] = update(sums[i + j], was[i + j]);
+                    mx_store8(mine + 32 * slab + i, x);
+                }
+            }
+            return;
+        }
+        if (32 * slab >= cols || rows == 0) return;
+        __syncwarp();
+#pragma unroll
+        for (uint32_t i = 0; i < 32; ++i) buf[lane * 33 + i] = __uint_as_float(sums[i]);
+        __syncwarp();
+        const bool in = 32 * slab + lane < cols;
+        float* to = at + 32 * slab + lane;
+#pragma unroll 1
+        for (uint32_t i0 = 0; i0 < rows; i0 += 8, to += 8 * ld) { // eight rows' loads before their stores: the compiler cannot tell that they are not the same place
+            float x[8], old[8];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                x[i] = buf[(i0 + i) * 33 + lane];
+                old[i] = beta != 0.f && in && i0 + i < rows ? to[i * ld] : 0.f;
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i)
+                if (in && i0 + i < rows) to[i * ld] = update(__float_as_uint(x[i]), old[i]);
+        }
+    }
+};
+
+// The scales of two blocks of four for this lane's quarter: a line of each 32, 16 bytes.  0 where there are none.
+__device__ __forceinline__ uint4 mx_scale_words(const uint8_t* tile, uint32_t chunk, uint32_t chunks, bool have, uint32_t lane) {
+    return have && chunk < chunks ? __ldg(reinterpret_cast<const uint4*>(tile + (uint64_t)chunk * 512) + lane) : make_uint4(0, 0, 0, 0);
+}
+
+__global__ void __launch_bounds__(kMxProductThreads, 2)
 k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MxProduct p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t s_bar[2 * kMxStages + 1];
+    __shared__ __align__(8) uint64_t s_bar[3 * kMxStages + 1];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t warp = warp_number(), lane = threadIdx.x & 31;
     const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    float* slabs = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)));
-    auto full = [&](uint32_t s) { return bar + 8 * s; };
-    auto empty = [&](uint32_t s) { return bar + 8 * (kMxStages + s); };
-    const uint32_t done = bar + 8 * (2 * kMxStages);
+    const uint32_t full = bar, empty = bar + 8 * kMxStages, scaled = bar + 16 * kMxStages, done = bar + 24 * kMxStages; // a stage's copies, products, scales; all products
+    if (warp == 4 && lane == 0 && p.a.blocks) { tma_prefetch(&map_a); tma_prefetch(&map_b); }
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < kMxStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (uint32_t s = 0; s < kMxStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); mbar_init(scaled + 8 * s, 4); }
         mbar_init(done, 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -126,62 +220,85 @@ k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     const uint32_t n = blockIdx.x / p.b.line_tiles / p.a.line_tiles;
     const uint32_t rounds = (p.a.blocks + kMxStageK / kMxBlock - 1) / (kMxStageK / kMxBlock), tiles = p.a.block_tiles;
     uint32_t r = 0; // rounds whose copies, or whose products, have been issued
-    if (warp == 4 && lane == 0) {
-        const uint8_t* sa = p.scales_a + ((uint64_t)n * p.a.line_tiles + at) * tiles * 512;
-        const uint8_t* sb = p.scales_b + ((uint64_t)n * p.b.line_tiles + bt) * tiles * 512;
-        for (; r < rounds; ++r) {
-            const uint32_t s = r % kMxStages, to = smem + s * kMxStageBytes;
-            if (r >= kMxStages && !mbar_wait(empty(s), (r / kMxStages - 1) & 1u, &s_failed)) break;
-            const uint32_t scale_bytes = min(tiles - 2 * r, 2u) * 512u;
-            mbar_expect(full(s), 2 * kMxOperandStage + 2 * scale_bytes);
-            tma_load_3d(to, &map_a, (int)(r * 128), (int)(at * kMxTile), (int)n, full(s));
-            tma_load_3d(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(bt * kMxTile), (int)n, full(s));
-            bulk_load(to + 2 * kMxOperandStage, sa + (uint64_t)r * 1024, scale_bytes, full(s));
-            bulk_load(to + 2 * kMxOperandStage + kMxScaleStage, sb + (uint64_t)r * 1024, scale_bytes, full(s));
+    if (warp == 4) {
+        MxRing<kMxStages> q;
+        for (; r < rounds; ++r, q.next()) {
+            const uint32_t to = smem + q.s * kMxStageBytes, ready = full + 8 * q.s;
+            if (r >= kMxStages && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
+            if (one_lane()) {
+                mbar_expect(ready, kMxStageBytes);
+                tma_load_3d(to, &map_a, (int)(r * 128), (int)(at * kMxTile), (int)n, ready);
+                tma_load_3d(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(bt * kMxTile), (int)n, ready);
+            }
         }
-    } else if (warp == 5 && lane == 0) {
-        for (; r < rounds; ++r) {
-            const uint32_t s = r % kMxStages, from = smem + s * kMxStageBytes, scales = tmem + 128 + 16 * s;
-            if (!mbar_wait(full(s), (r / kMxStages) & 1u, &s_failed)) break;
+    } else if (warp == 5) {
+        MxRing<kMxStages> q;
+        for (; r < rounds; ++r, q.next()) {
+            const uint32_t scales = tmem + kMxTile + 16 * q.s;
+            const uint64_t a = mx_desc_codes(smem + q.s * kMxStageBytes), b = mx_desc_codes(smem + q.s * kMxStageBytes + kMxOperandStage);
+            if (!mbar_wait(scaled + 8 * q.s, q.parity, &s_failed)) break; // ... which the warps that stored them have waited for `full` with
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t products = min((p.a.blocks - r * 8 + 1) / 2, 4u); // of 64 values, two blocks, each
-            for (uint32_t t = 0; 2 * t < products; ++t) {
-                tc_copy_scales(scales + 4 * t, mx_desc_scales(from + 2 * kMxOperandStage + 512 * t));
-                tc_copy_scales(scales + 8 + 4 * t, mx_desc_scales(from + 2 * kMxOperandStage + kMxScaleStage + 512 * t));
+            if (one_lane()) {
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k)
+                    if (k < products) tc_mma_mxf4<1>(tmem, a + 2 * k, b + 2 * k, mx_idesc(128, 128, k & 1u), scales + 4 * (k >> 1), scales + 8 + 4 * (k >> 1), r + k > 0);
+                tc_commit<1>(empty + 8 * q.s);
             }
-            for (uint32_t k = 0; k < products; ++k)
-                tc_mma_mxf4(tmem, mx_desc_codes(from + 32 * k), mx_desc_codes(from + kMxOperandStage + 32 * k), mx_idesc(k & 1u), scales + 4 * (k >> 1),
-                            scales + 8 + 4 * (k >> 1), r + k > 0);
-            tc_commit(empty(s));
         }
-        tc_commit(done);
+        if (one_lane()) tc_commit<1>(done);
     }
     __syncwarp();
     if (warp < 4) {
+        const MxOutput o(p, n, at * kMxTile + warp * 32, bt * kMxTile, kMxTile, lane);
+        float* buf = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw))) + warp * 32 * 33;
+        const uint8_t* sa = p.scales_a + ((uint64_t)n * p.a.line_tiles + at) * tiles * 512;
+        const uint8_t* sb = p.scales_b + ((uint64_t)n * p.b.line_tiles + bt) * tiles * 512;
+        const uint32_t mine = tmem + (warp * 32 << 16);
+        float was[2][32];
+        o.fetch(0, was[0]);
+        o.fetch(1, was[1]);
+        auto load = [&](uint32_t r, uint4 (&v)[4]) {
+#pragma unroll
+            for (uint32_t k = 0; k < 2; ++k) {
+                v[k] = mx_scale_words(sa, 2 * r + k, tiles, true, lane);
+                v[2 + k] = mx_scale_words(sb, 2 * r + k, tiles, true, lane);
+            }
+        };
+        MxRing<kMxStages> q;
+        auto store = [&](const uint4 (&v)[4]) {
+            if (!mbar_wait(full + 8 * q.s, q.parity, &s_failed)) return false; // (and so the products that used the scales' place before are done)
+            __syncwarp();
+            tc_store16(mine + kMxTile + 16 * q.s, v);
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (one_lane()) mbar_arrive(scaled + 8 * q.s);
+            q.next();
+            return true;
+        };
+        uint4 v0[4], v1[4]; // two rounds under way
+        load(0, v0);
+        load(1, v1);
+        for (uint32_t r = 0; r < rounds; r += 2) {
+            if (!store(v0)) break;
+            load(r + 2, v0);
+            if (r + 1 >= rounds || !store(v1)) break;
+            load(r + 3, v1);
+        }
         const bool fine = mbar_wait(done, 0, &s_failed) && !s_failed;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        __syncwarp();
         if (fine) {
-            float* slab = slabs + warp * 32 * 33;
-            const uint32_t row0 = at * kMxTile + warp * 32, col0 = bt * kMxTile;
-            float* out = p.out + n * p.batch_stride + (uint64_t)row0 * p.ld + col0;
-            const uint32_t rows = row0 < p.a.lines ? min(p.a.lines - row0, 32u) : 0u;
-            for (uint32_t c = 0; c < kMxTile && col0 + c < p.b.lines; c += 32) {
-                uint32_t v[32];
-                if (rounds) tc_load32(v, tmem + (warp * 32 << 16) + c);
-                __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) slab[lane * 33 + i] = rounds ? __uint_as_float(v[i]) : 0.f;
-                __syncwarp();
-                const bool in = col0 + c + lane < p.b.lines;
-                float was[32];
+            for (uint32_t slab = 0; slab < 4; ++slab) {
+                uint32_t sums[32];
+                if (rounds) tc_load32(sums, mine + 32 * slab);
+                else {
 #pragma unroll
-                for (uint32_t i = 0; i < 32; ++i) was[i] = p.beta != 0.f && in && i < rows ? out[i * p.ld + c + lane] : 0.f;
-#pragma unroll
-                for (uint32_t i = 0; i < 32; ++i) {
-                    float x = __fmul_rn(p.alpha, slab[i * 33 + lane]);
-                    if (p.beta != 0.f) x = __fmaf_rn(p.beta, was[i], x);
-                    if (in && i < rows) out[i * p.ld + c + lane] = x;
+                    for (int i = 0; i < 32; ++i) sums[i] = 0;
                 }
+                o.put(slab, sums, was[slab & 1], buf);
+                if (slab < 2) o.fetch(slab + 2, was[slab & 1]);
             }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -192,7 +309,7 @@ k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         const long long began = clock64();
         if (warp == 4 && lane == 0)
             for (uint32_t i = r > kMxStages ? r - kMxStages : 0; i < r; ++i)
-                while (!mbar_try(full(i % kMxStages), (i / kMxStages) & 1u) && clock64() - began < kMxWaitClocks) {}
+                while (!mbar_try(full + 8 * (i % kMxStages), (i / kMxStages) & 1u) && clock64() - began < kMxWaitClocks) {}
         if (warp == 5 && lane == 0)
             while (!mbar_try(done, 0) && clock64() - began < kMxWaitClocks) {}
         __syncwarp();
@@ -200,6 +317,219 @@ k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     if (warp == 5) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kMxTmemCols) : "memory");
+    }
+}
+
+// ---- Pairs.  Where there are enough tiles, two CTAs (SMs) take tiles of 256 by kMxPairN together (cta_group::2): each holds 128 of A's lines and half of
+// B's in shared memory, and both tensor cores read both halves.  An SM then reads 28 KB of codes per 256 values of a tile of 128 by 192 sums, where 128 by
+// 128 alone needs 32: an SM takes 64 bytes per clock from L2, so a tile alone runs at half the products' rate at most.
+// One CTA per SM stays for all its tiles; the sums are held twice, so that one tile's outputs are written beside the next one's products.
+// Warps: 0-7 outputs (a quarter of the lines and half of the columns each), 8-11 scales, 12 copies, 13 products (in the pair's first CTA).
+constexpr uint32_t kMxPairN = 192;
+constexpr uint32_t kMxPairStages = 5;
+constexpr uint32_t kMxPairBytesB = kMxPairN / 2 * 128;
+constexpr uint32_t kMxPairStageBytes = kMxOperandStage + kMxPairBytesB;
+constexpr uint32_t kMxPairSlabs = 8 * 32 * 33 * 4;
+constexpr uint32_t kMxPairSmem = 1024 + kMxPairStages * kMxPairStageBytes + kMxPairSlabs;
+constexpr int kMxPairThreads = 448;
+constexpr uint32_t kMxPairScaleCols = 24; // of a stage: A's 2 x 4, B's 2 x 8 (6 in use)
+static_assert(2 * kMxPairN + kMxPairStages * kMxPairScaleCols <= 512, "tensor memory");
+static_assert(kMxPairSmem <= 227 * 1024 && kMxPairStageBytes % 1024 == 0 && kMxPairN == 192, "shared memory; tc_store_scales");
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// Arrival on the barrier of the pair's first CTA.  Relaxed: what is handed over are accesses to tensor memory that have been waited for (tcgen05.wait) and
+// copies that have been, none of the thread's own writes; with release the arrival waits for every store under way, about 1000 clocks.
+__device__ __forceinline__ void mbar_arrive_first(uint32_t bar) {
+    asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %0, 0;\nmbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [a];\n}" ::"r"(bar) : "memory");
+}
+// A's eight words, and B's twelve at columns 8-13 and 16-21.
+__device__ __forceinline__ void tc_store_scales(uint32_t addr, const uint4 (&a)[2], const uint2 (&b)[6]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(a[0].x), "r"(a[0].y), "r"(a[0].z), "r"(a[0].w), "r"(a[1].x),
+                 "r"(a[1].y), "r"(a[1].z), "r"(a[1].w) : "memory");
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%13,%13,%7,%8,%9,%10,%11,%12,%13,%13};" ::"r"(addr + 8), "r"(b[0].x), "r"(b[0].y),
+                 "r"(b[1].x), "r"(b[1].y), "r"(b[2].x), "r"(b[2].y), "r"(b[3].x), "r"(b[3].y), "r"(b[4].x), "r"(b[4].y), "r"(b[5].x), "r"(b[5].y), "r"(0) : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+struct MxPairTile {
+    uint32_t row, col; // first output
+    uint32_t n;        // matrix
+    __device__ __forceinline__ MxPairTile(const MxProduct& p, uint32_t tile) {
+        const uint32_t across = (p.b.lines + kMxPairN - 1) / kMxPairN, down = (p.a.lines + 255) / 256;
+        col = tile % across * kMxPairN;
+        row = tile / across % down * 256;
+        n = tile / across / down;
+    }
+};
+
+__global__ void __launch_bounds__(kMxPairThreads, 1) __cluster_dims__(2, 1, 1)
+k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MxProduct p, uint32_t all_tiles) {
+    extern __shared__ uint8_t smem_raw[];
+    constexpr uint32_t S = kMxPairStages;
+    __shared__ __align__(8) uint64_t s_bar[3 * S + 5];
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile uint32_t s_failed;
+    const uint32_t warp = warp_number(), lane = threadIdx.x & 31, rank = cluster_rank();
+    const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    // a stage's copies are here; its scales are in tensor memory, in both CTAs (first CTA); its products are done; a tile's products are done; its sums
+    // have been read, in both CTAs (first CTA); everything issued is done
+    const uint32_t full = bar, ready = bar + 8 * S, empty = bar + 16 * S, done = bar + 24 * S, drained = done + 16, quit = done + 32;
+    if (warp == 12 && lane == 0) { tma_prefetch(&map_a); tma_prefetch(&map_b); }
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 1); mbar_init(ready + 8 * s, 8); mbar_init(empty + 8 * s, 1); }
+        for (uint32_t b = 0; b < 2; ++b) { mbar_init(done + 8 * b, 1); mbar_init(drained + 8 * b, 16); }
+        mbar_init(quit, 1);
+        s_failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 13) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    pdl_wait();
+
+    const uint32_t pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const uint32_t rounds = (p.a.blocks + kMxStageK / kMxBlock - 1) / (kMxStageK / kMxBlock), tiles = p.a.block_tiles;
+    uint32_t it = 0; // stages whose copies, or whose products, have been issued
+    MxRing<S> q;
+    if (warp == 12) {
+        for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
+            const MxPairTile t(p, tile);
+            for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
+                const uint32_t to = smem + q.s * kMxPairStageBytes, here = full + 8 * q.s;
+                if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
+                if (one_lane()) {
+                    mbar_expect(here, kMxPairStageBytes);
+                    tma_load_3d(to, &map_a, (int)(r * 128), (int)(t.row + rank * kMxTile), (int)t.n, here);
+                    tma_load_3d(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(t.col + rank * (kMxPairN / 2)), (int)t.n, here);
+                }
+            }
+        }
+    } else if (warp == 13 && rank == 0) {
+        MxRing<2> u; // places of sums
+        uint32_t j = 0; // tiles of this pair
+        for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs, ++j, u.next()) {
+            const uint32_t sums = tmem + u.s * kMxPairN;
+            if (j >= 2 && !mbar_wait(drained + 8 * u.s, u.parity ^ 1u, &s_failed)) break;
+            for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
+                const uint32_t scales = tmem + 2 * kMxPairN + kMxPairScaleCols * q.s;
+                const uint64_t a = mx_desc_codes(smem + q.s * kMxPairStageBytes), b = mx_desc_codes(smem + q.s * kMxPairStageBytes + kMxOperandStage);
+                const uint32_t products = min((p.a.blocks - r * 8 + 1) / 2, 4u); // of 64 values, two blocks, each
+                if (!mbar_wait(ready + 8 * q.s, q.parity, &s_failed)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (one_lane()) {
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k)
+                        if (k < products)
+                            tc_mma_mxf4<2>(sums, a + 2 * k, b + 2 * k, mx_idesc(256, kMxPairN, k & 1u), scales + 4 * (k >> 1), scales + 8 + 8 * (k >> 1), r + k > 0);
+                    tc_commit<2>(empty + 8 * q.s);
+                }
+            }
+            if (one_lane()) tc_commit<2>(done + 8 * u.s);
+        }
+        if (s_failed && one_lane()) tc_commit<2>(quit);
+    } else if (warp >= 8 && warp < 12) {
+        const uint32_t mine = tmem + ((warp - 8) * 32 << 16) + 2 * kMxPairN;
+        for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
+            const MxPairTile t(p, tile);
+            const uint32_t la = t.row / kMxTile + rank, lb = t.col / kMxTile; // tiles of lines whose scales these are
+            const bool have_a = la < p.a.line_tiles, have_b = lb + 1 < p.b.line_tiles, second = t.col % kMxTile != 0; // B's lines start with a tile's second half
+            // this lane's words of A's tile, and of B's lines 64 by 64: two words each
+            const uint8_t* from_a = p.scales_a + ((uint64_t)t.n * p.a.line_tiles + la) * tiles * 512 + lane * 16;
+            const uint8_t* from_b0 = p.scales_b + ((uint64_t)t.n * p.b.line_tiles + lb) * tiles * 512 + lane * 16 + second * 8;
+            const uint8_t* from_b1 = second ? from_b0 + (uint64_t)tiles * 512 - 8 : from_b0 + 8;
+            const uint8_t* from_b2 = second ? from_b1 + 8 : from_b1 + (uint64_t)tiles * 512 - 8;
+            const bool have_b1 = have_b || !second;
+            auto load = [&](uint32_t r, uint4 (&a)[2], uint2 (&b)[6]) {
+#pragma unroll
+                for (uint32_t k = 0; k < 2; ++k) {
+                    const bool in = 2 * r + k < tiles;
+                    const uint64_t off = (uint64_t)(2 * r + k) * 512;
+                    a[k] = in && have_a ? __ldg(reinterpret_cast<const uint4*>(from_a + off)) : make_uint4(0, 0, 0, 0);
+                    b[3 * k] = in ? __ldg(reinterpret_cast<const uint2*>(from_b0 + off)) : make_uint2(0, 0);
+                    b[3 * k + 1] = in && have_b1 ? __ldg(reinterpret_cast<const uint2*>(from_b1 + off)) : make_uint2(0, 0);
+                    b[3 * k + 2] = in && have_b ? __ldg(reinterpret_cast<const uint2*>(from_b2 + off)) : make_uint2(0, 0);
+                }
+            };
+            auto store = [&](const uint4 (&a)[2], const uint2 (&b)[6]) {
+                if (!mbar_wait(full + 8 * q.s, q.parity, &s_failed)) return false; // (and so the products that used the scales' place before are done)
+                __syncwarp();
+                tc_store_scales(mine + kMxPairScaleCols * q.s, a, b);
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (one_lane()) mbar_arrive_first(ready + 8 * q.s);
+                q.next();
+                return true;
+            };
+            uint4 a0[2], a1[2];
+            uint2 b0[6], b1[6]; // two rounds under way
+            load(0, a0, b0);
+            load(1, a1, b1);
+            for (uint32_t r = 0; r < rounds; r += 2) {
+                if (!store(a0, b0)) break;
+                load(r + 2, a0, b0);
+                if (r + 1 >= rounds || !store(a1, b1)) break;
+                load(r + 3, a1, b1);
+            }
+        }
+    }
+    __syncwarp();
+    if (warp < 8) {
+        const uint32_t quarter = warp & 3u, half = warp >> 2;
+        float* buf = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + S * kMxPairStageBytes) + warp * 32 * 33;
+        uint32_t j = 0;
+        for (uint32_t tile = pair; tile < all_tiles; tile += pairs, ++j) {
+            const MxPairTile t(p, tile);
+            const uint32_t b = j & 1u, sums_at = tmem + (quarter * 32 << 16) + b * kMxPairN + half * (kMxPairN / 2);
+            const MxOutput o(p, t.n, t.row + rank * kMxTile + quarter * 32, t.col + half * (kMxPairN / 2), kMxPairN / 2, lane);
+            float was[2][32];
+            o.fetch(0, was[0]);
+            o.fetch(1, was[1]);
+            if (!mbar_wait(done + 8 * b, (j / 2) & 1u, &s_failed) || s_failed) break;
+            __syncwarp();
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (uint32_t slab = 0; slab < kMxPairN / 64; ++slab) {
+                uint32_t sums[32];
+                tc_load32(sums, sums_at + 32 * slab);
+                if (slab == kMxPairN / 64 - 1) { // the sums' place is free again
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (one_lane()) mbar_arrive_first(drained + 8 * b);
+                }
+                o.put(slab, sums, was[slab & 1], buf);
+                if (slab + 2 < kMxPairN / 64) o.fetch(slab + 2, was[slab & 1]);
+            }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    __syncthreads();
+    if (s_failed) { // what was issued still writes to the pair's shared and tensor memory
+        if (threadIdx.x == 0 && p.status) *p.status = KIMAD_ERR_TIMEOUT;
+        const long long began = clock64();
+        if (warp == 12 && lane == 0)
+            for (uint32_t i = it > S ? it - S : 0; i < it; ++i)
+                while (!mbar_try(full + 8 * (i % S), (i / S) & 1u) && clock64() - began < kMxWaitClocks) {}
+        if (warp == 13 && lane == 0 && rank == 0)
+            while (!mbar_try(quit, 0) && clock64() - began < kMxWaitClocks) {}
+        __syncwarp();
+    }
+    cluster_sync(); // neither CTA's memory goes before both are through with it
+    if (warp == 13) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
 }
 

@@ -45,7 +45,9 @@ def exact_matrix(shape, rng):
 
 
 SHAPES = [(1, 1, 1, 1), (1, 128, 128, 64), (1, 128, 128, 256), (1, 7, 300, 33), (1, 300, 7, 65), (2, 129, 127, 31), (3, 64, 257, 97), (1, 130, 131, 129),
-          (1, 256, 384, 1000), (4, 20, 30, 511), (1, 1, 1000, 257), (2, 513, 1, 768), (1, 128, 128, 800)]
+          (1, 256, 384, 1000), (4, 20, 30, 511), (1, 1, 1000, 257), (2, 513, 1, 768), (1, 128, 128, 800),
+          # enough tiles of 256 x 192 for pairs of SMs: whole and cut in every direction, more tiles than pairs, more rounds than stages
+          (1, 2560, 1536, 64), (40, 130, 200, 300), (80, 20, 30, 511), (1, 2500, 2000, 33), (3, 1300, 1000, 1000), (19, 257, 193, 900), (76, 256, 192, 256)]
 
 
 @pytest.mark.parametrize("batch,m,n,length", SHAPES)
@@ -68,7 +70,7 @@ def test_exact_sums(batch, m, n, length):
         assert np.array_equal(out.cpu().numpy().astype(np.float64), 0.5 * want - 2.0 * was)
 
 
-@pytest.mark.parametrize("batch,m,n,length", [(1, 200, 150, 5), (2, 130, 70, 777), (1, 256, 300, 4096), (1, 33, 65, 9000)])
+@pytest.mark.parametrize("batch,m,n,length", [(1, 200, 150, 5), (2, 130, 70, 777), (1, 256, 300, 4096), (1, 33, 65, 9000), (1, 2304, 1600, 4500)])
 def test_sums_of_any_values(batch, m, n, length):
     """Bound: at most one rounding (by less than a step of the binary32 result, 2^-23 of what has been added up so far in magnitude) per 32 values, and
     one each for alpha, beta."""
