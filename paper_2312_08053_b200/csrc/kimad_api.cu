@@ -1163,6 +1163,16 @@ bool mx4_map(CUtensorMap* map, const uint8_t* codes, const MxOperand& op, uint64
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The output in slabs of 32 by 32, where it lies on 16 bytes; false where it does not.
+bool mx4_map_output(CUtensorMap* map, float* out, uint64_t m, uint64_t n, uint64_t batch, uint64_t ld, uint64_t batch_stride) {
+    if ((uintptr_t)out % 16 || ld % 4 || (batch > 1 && batch_stride % 4) || ld >= 1ull << 38 || (batch > 1 && batch_stride >= 1ull << 38)) return false;
+    const cuuint64_t dims[3] = {n, m, batch}, strides[2] = {ld * 4, (batch > 1 ? batch_stride : ld) * 4};
+    const cuuint32_t box[3] = {32, 32, 1}, each[3] = {1, 1, 1};
+    const EncodeTiled encode = encode_tiled();
+    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, out, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 } // namespace
 extern "C" {
 
@@ -1302,8 +1312,10 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
         return KIMAD_ERR_CUDA;
     { const int rc = mx4_prepare_product(); if (rc != KIMAD_OK) return rc; }
     if (pairs) {
-        CUDA_TRY(launch_pdl(k_mx4_product_pairs, dim3((uint32_t)std::min<uint64_t>(pair_tiles, 74) * 2), kMxPairThreads, kMxPairSmem, s, map_a, map_b, p,
-                            (uint32_t)pair_tiles));
+        CUtensorMap map_out{};
+        const uint32_t by_tma = mx4_map_output(&map_out, out_dev, m, n, batch, ld, batch_stride);
+        CUDA_TRY(launch_pdl(k_mx4_product_pairs, dim3((uint32_t)std::min<uint64_t>(pair_tiles, 74) * 2), kMxPairThreads, kMxPairSmem, s, map_a, map_b,
+                            map_out, p, (uint32_t)pair_tiles, by_tma));
         CUDA_TRY(cudaGetLastError());
         return KIMAD_OK;
     }

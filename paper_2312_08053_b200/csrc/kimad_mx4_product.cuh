@@ -62,6 +62,9 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x),
                  "r"(y), "r"(z), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void tc_store16(uint32_t addr, const uint4 (&v)[4]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(v[0].x), "r"(v[0].y),
@@ -69,6 +72,13 @@ __device__ __forceinline__ void tc_store16(uint32_t addr, const uint4 (&v)[4]) {
                  "r"(v[3].y), "r"(v[3].z), "r"(v[3].w) : "memory");
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// All but the `most` latest stores of this thread have read their memory.
+template <int most> __device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(most) : "memory"); }
+__device__ __forceinline__ void tma_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // GROUP: CTAs whose tensor cores take one product together.
 template <int GROUP> __device__ __forceinline__ void tc_mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
     if (GROUP == 1)
@@ -163,6 +173,9 @@ struct MxOutput {
             }
             return;
         }
+        put_any(slab, sums, buf);
+    }
+    __device__ __forceinline__ void put_any(uint32_t slab, const uint32_t (&sums)[32], float* buf) const {
         if (32 * slab >= cols || rows == 0) return;
         __syncwarp();
 #pragma unroll
@@ -323,14 +336,17 @@ k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
 // ---- Pairs.  Where there are enough tiles, two CTAs (SMs) take tiles of 256 by kMxPairN together (cta_group::2): each holds 128 of A's lines and half of
 // B's in shared memory, and both tensor cores read both halves.  An SM then reads 28 KB of codes per 256 values of a tile of 128 by 192 sums, where 128 by
 // 128 alone needs 32: an SM takes 64 bytes per clock from L2, so a tile alone runs at half the products' rate at most.
-// One CTA per SM stays for all its tiles; the sums are held twice, so that one tile's outputs are written beside the next one's products.
+// One CTA per SM stays for all its tiles; the sums are held twice, so that one tile's outputs are written beside the next one's products.  Outputs
+// on 16 bytes come and go by TMA, slab by slab: the stores of eight warps are more than an SM gets rid of at once (about 16 bytes per clock when all
+// write), and what waits in line behind them are the other warps' barriers, scales and products (stages took 2000 clocks beside them, 480 otherwise).
 // Warps: 0-7 outputs (a quarter of the lines and half of the columns each), 8-11 scales, 12 copies, 13 products (in the pair's first CTA).
 constexpr uint32_t kMxPairN = 192;
 constexpr uint32_t kMxPairStages = 5;
 constexpr uint32_t kMxPairBytesB = kMxPairN / 2 * 128;
-constexpr uint32_t kMxPairStageBytes = kMxOperandStage + kMxPairBytesB;
-constexpr uint32_t kMxPairSlabs = 8 * 32 * 33 * 4;
-constexpr uint32_t kMxPairSmem = 1024 + kMxPairStages * kMxPairStageBytes + kMxPairSlabs;
+constexpr uint32_t kMxPairScales = 2 * 512; // bytes of a stage's scales of a tile of lines; of A's one and of B's two
+constexpr uint32_t kMxPairStageBytes = kMxOperandStage + kMxPairBytesB + 3 * kMxPairScales;
+constexpr uint32_t kMxPairOut = 2 * 4096; // bytes of a warp's outputs: two slabs of 32 by 32, or one of 32 by 33
+constexpr uint32_t kMxPairSmem = 1024 + kMxPairStages * kMxPairStageBytes + 8 * kMxPairOut;
 constexpr int kMxPairThreads = 448;
 constexpr uint32_t kMxPairScaleCols = 24; // of a stage: A's 2 x 4, B's 2 x 8 (6 in use)
 static_assert(2 * kMxPairN + kMxPairStages * kMxPairScaleCols <= 512, "tensor memory");
@@ -348,6 +364,16 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 // copies that have been, none of the thread's own writes; with release the arrival waits for every store under way, about 1000 clocks.
 __device__ __forceinline__ void mbar_arrive_first(uint32_t bar) {
     asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %0, 0;\nmbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [a];\n}" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint4 shared4(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 shared2(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
 }
 // A's eight words, and B's twelve at columns 8-13 and 16-21.
 __device__ __forceinline__ void tc_store_scales(uint32_t addr, const uint4 (&a)[2], const uint2 (&b)[6]) {
@@ -370,22 +396,29 @@ struct MxPairTile {
 };
 
 __global__ void __launch_bounds__(kMxPairThreads, 1) __cluster_dims__(2, 1, 1)
-k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MxProduct p, uint32_t all_tiles) {
+k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+                    const __grid_constant__ MxProduct p, uint32_t all_tiles, uint32_t by_tma) {
     extern __shared__ uint8_t smem_raw[];
     constexpr uint32_t S = kMxPairStages;
-    __shared__ __align__(8) uint64_t s_bar[3 * S + 5];
+    __shared__ __align__(8) uint64_t s_bar[3 * S + 5 + 16];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
     const uint32_t warp = warp_number(), lane = threadIdx.x & 31, rank = cluster_rank();
     const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // a stage's copies are here; its scales are in tensor memory, in both CTAs (first CTA); its products are done; a tile's products are done; its sums
     // have been read, in both CTAs (first CTA); everything issued is done
-    const uint32_t full = bar, ready = bar + 8 * S, empty = bar + 16 * S, done = bar + 24 * S, drained = done + 16, quit = done + 32;
-    if (warp == 12 && lane == 0) { tma_prefetch(&map_a); tma_prefetch(&map_b); }
+    const uint32_t full = bar, ready = bar + 8 * S, empty = bar + 16 * S, done = bar + 24 * S, drained = done + 16, quit = done + 32,
+                   old = quit + 8; // (an output warp's slabs of old values: two each)
+    if (warp == 12 && one_lane()) {
+        tma_prefetch(&map_a);
+        tma_prefetch(&map_b);
+        if (by_tma) tma_prefetch(&map_out);
+    }
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 1); mbar_init(ready + 8 * s, 8); mbar_init(empty + 8 * s, 1); }
         for (uint32_t b = 0; b < 2; ++b) { mbar_init(done + 8 * b, 1); mbar_init(drained + 8 * b, 16); }
         mbar_init(quit, 1);
+        for (uint32_t i = 0; i < 16; ++i) mbar_init(old + 8 * i, 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -407,11 +440,19 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (warp == 12) {
         for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
             const MxPairTile t(p, tile);
+            const uint32_t la = t.row / kMxTile + rank, lb = t.col / kMxTile; // tiles of lines whose scales are read
+            const bool have_a = la < p.a.line_tiles, have_b = lb + 1 < p.b.line_tiles;
+            const uint8_t* sa = p.scales_a + ((uint64_t)t.n * p.a.line_tiles + la) * tiles * 512;
+            const uint8_t* sb = p.scales_b + ((uint64_t)t.n * p.b.line_tiles + lb) * tiles * 512;
             for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
-                const uint32_t to = smem + q.s * kMxPairStageBytes, here = full + 8 * q.s;
+                const uint32_t to = smem + q.s * kMxPairStageBytes, here = full + 8 * q.s, scales = to + kMxOperandStage + kMxPairBytesB;
                 if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
                 if (one_lane()) {
-                    mbar_expect(here, kMxPairStageBytes);
+                    const uint32_t bytes = min(tiles - 2 * r, 2u) * 512u;
+                    mbar_expect(here, kMxOperandStage + kMxPairBytesB + bytes * (1u + have_a + have_b));
+                    if (have_a) bulk_load(scales, sa + (uint64_t)r * 1024, bytes, here);
+                    bulk_load(scales + kMxPairScales, sb + (uint64_t)r * 1024, bytes, here);
+                    if (have_b) bulk_load(scales + 2 * kMxPairScales, sb + (uint64_t)tiles * 512 + (uint64_t)r * 1024, bytes, here);
                     tma_load_3d(to, &map_a, (int)(r * 128), (int)(t.row + rank * kMxTile), (int)t.n, here);
                     tma_load_3d(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(t.col + rank * (kMxPairN / 2)), (int)t.n, here);
                 }
@@ -444,75 +485,101 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         const uint32_t mine = tmem + ((warp - 8) * 32 << 16) + 2 * kMxPairN;
         for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
             const MxPairTile t(p, tile);
-            const uint32_t la = t.row / kMxTile + rank, lb = t.col / kMxTile; // tiles of lines whose scales these are
-            const bool have_a = la < p.a.line_tiles, have_b = lb + 1 < p.b.line_tiles, second = t.col % kMxTile != 0; // B's lines start with a tile's second half
-            // this lane's words of A's tile, and of B's lines 64 by 64: two words each
-            const uint8_t* from_a = p.scales_a + ((uint64_t)t.n * p.a.line_tiles + la) * tiles * 512 + lane * 16;
-            const uint8_t* from_b0 = p.scales_b + ((uint64_t)t.n * p.b.line_tiles + lb) * tiles * 512 + lane * 16 + second * 8;
-            const uint8_t* from_b1 = second ? from_b0 + (uint64_t)tiles * 512 - 8 : from_b0 + 8;
-            const uint8_t* from_b2 = second ? from_b1 + 8 : from_b1 + (uint64_t)tiles * 512 - 8;
-            const bool have_b1 = have_b || !second;
-            auto load = [&](uint32_t r, uint4 (&a)[2], uint2 (&b)[6]) {
+            // this lane's words of B's lines, 64 by 64: the first ones may be a tile's second half
+            const uint32_t b0 = kMxPairScales + t.col % kMxTile / 64 * 8, b1 = b0 & 8u ? 2 * kMxPairScales : b0 + 8, b2 = b0 & 8u ? b1 + 8 : 2 * kMxPairScales;
+            for (uint32_t r = 0; r < rounds; ++r, q.next()) {
+                const uint32_t from = smem + q.s * kMxPairStageBytes + kMxOperandStage + kMxPairBytesB + lane * 16;
+                if (!mbar_wait(full + 8 * q.s, q.parity, &s_failed)) break; // (and so the products that used the scales' place before are done)
+                uint4 a[2];
+                uint2 b[6];
 #pragma unroll
                 for (uint32_t k = 0; k < 2; ++k) {
-                    const bool in = 2 * r + k < tiles;
-                    const uint64_t off = (uint64_t)(2 * r + k) * 512;
-                    a[k] = in && have_a ? __ldg(reinterpret_cast<const uint4*>(from_a + off)) : make_uint4(0, 0, 0, 0);
-                    b[3 * k] = in ? __ldg(reinterpret_cast<const uint2*>(from_b0 + off)) : make_uint2(0, 0);
-                    b[3 * k + 1] = in && have_b1 ? __ldg(reinterpret_cast<const uint2*>(from_b1 + off)) : make_uint2(0, 0);
-                    b[3 * k + 2] = in && have_b ? __ldg(reinterpret_cast<const uint2*>(from_b2 + off)) : make_uint2(0, 0);
+                    a[k] = shared4(from + 512 * k);
+                    b[3 * k] = shared2(from + 512 * k + b0);
+                    b[3 * k + 1] = shared2(from + 512 * k + b1);
+                    b[3 * k + 2] = shared2(from + 512 * k + b2);
                 }
-            };
-            auto store = [&](const uint4 (&a)[2], const uint2 (&b)[6]) {
-                if (!mbar_wait(full + 8 * q.s, q.parity, &s_failed)) return false; // (and so the products that used the scales' place before are done)
                 __syncwarp();
                 tc_store_scales(mine + kMxPairScaleCols * q.s, a, b);
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (one_lane()) mbar_arrive_first(ready + 8 * q.s);
-                q.next();
-                return true;
-            };
-            uint4 a0[2], a1[2];
-            uint2 b0[6], b1[6]; // two rounds under way
-            load(0, a0, b0);
-            load(1, a1, b1);
-            for (uint32_t r = 0; r < rounds; r += 2) {
-                if (!store(a0, b0)) break;
-                load(r + 2, a0, b0);
-                if (r + 1 >= rounds || !store(a1, b1)) break;
-                load(r + 3, a1, b1);
             }
         }
     }
     __syncwarp();
     if (warp < 8) {
         const uint32_t quarter = warp & 3u, half = warp >> 2;
-        float* buf = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + S * kMxPairStageBytes) + warp * 32 * 33;
-        uint32_t j = 0;
-        for (uint32_t tile = pair; tile < all_tiles; tile += pairs, ++j) {
+        constexpr uint32_t kSlabs = kMxPairN / 64;
+        const uint32_t slabs = smem + S * kMxPairStageBytes + warp * kMxPairOut;
+        float* buf = reinterpret_cast<float*>(smem_raw + (slabs - smem_u32(smem_raw)));
+        MxRing<2> u;     // places of sums
+        MxRing<2> w, l;  // slabs worked on, slabs whose old values are asked for
+        for (uint32_t tile = pair; tile < all_tiles; tile += pairs, u.next()) {
             const MxPairTile t(p, tile);
-            const uint32_t b = j & 1u, sums_at = tmem + (quarter * 32 << 16) + b * kMxPairN + half * (kMxPairN / 2);
+            const uint32_t sums_at = tmem + (quarter * 32 << 16) + u.s * kMxPairN + half * (kMxPairN / 2);
             const MxOutput o(p, t.n, t.row + rank * kMxTile + quarter * 32, t.col + half * (kMxPairN / 2), kMxPairN / 2, lane);
-            float was[2][32];
-            o.fetch(0, was[0]);
-            o.fetch(1, was[1]);
-            if (!mbar_wait(done + 8 * b, (j / 2) & 1u, &s_failed) || s_failed) break;
+            const int row = (int)(t.row + rank * kMxTile + quarter * 32), col = (int)(t.col + half * (kMxPairN / 2));
+            const uint32_t mine = by_tma && o.rows ? (o.cols + 31) / 32 : 0u; // slabs by TMA
+            auto ask = [&](uint32_t slab) { // for a slab's old values, in a place whose last store has been read
+                if (lane == 0) {
+                    tma_stores_read<0>();
+                    mbar_expect(old + 8 * (2 * warp + l.s), 4096);
+                    tma_load_3d(slabs + 4096 * l.s, &map_out, col + 32 * (int)slab, row, (int)t.n, old + 8 * (2 * warp + l.s));
+                }
+                l.next();
+            };
+            if (p.beta != 0.f) {
+                if (mine > 0) ask(0);
+                if (mine > 1) ask(1);
+            }
+            if (!mbar_wait(done + 8 * u.s, u.parity, &s_failed) || s_failed) break;
             __syncwarp();
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-            for (uint32_t slab = 0; slab < kMxPairN / 64; ++slab) {
+            for (uint32_t slab = 0; slab < kSlabs; ++slab) {
                 uint32_t sums[32];
                 tc_load32(sums, sums_at + 32 * slab);
-                if (slab == kMxPairN / 64 - 1) { // the sums' place is free again
+                if (slab == kSlabs - 1) { // the sums' place is free again
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
-                    if (one_lane()) mbar_arrive_first(drained + 8 * b);
+                    if (one_lane()) mbar_arrive_first(drained + 8 * u.s);
                 }
-                o.put(slab, sums, was[slab & 1], buf);
-                if (slab + 2 < kMxPairN / 64) o.fetch(slab + 2, was[slab & 1]);
+                if (!by_tma) o.put_any(slab, sums, buf);
+                if (slab >= mine) continue;
+                // sixteen bytes c of row r lie at c ^ (r % 8): no two of eight lanes meet in a bank
+                const uint32_t at = slabs + 4096 * w.s + lane * 128;
+                if (p.beta != 0.f) {
+                    if (!mbar_wait(old + 8 * (2 * warp + w.s), w.parity, &s_failed)) break;
+                } else {
+                    if (lane == 0) tma_stores_read<1>(); // the other place's store may still be under way
+                }
+                __syncwarp();
+#pragma unroll
+                for (uint32_t c = 0; c < 8; ++c) {
+                    const uint32_t place = at + ((c ^ (lane & 7u)) << 4);
+                    float4 was = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (p.beta != 0.f) {
+                        const uint4 x = shared4(place);
+                        was = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
+                    }
+                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(place), "f"(o.update(sums[4 * c], was.x)), "f"(o.update(sums[4 * c + 1], was.y)),
+                                 "f"(o.update(sums[4 * c + 2], was.z)), "f"(o.update(sums[4 * c + 3], was.w)) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) tma_store_3d(&map_out, col + 32 * (int)slab, row, (int)t.n, slabs + 4096 * w.s);
+                w.next();
+                if (p.beta != 0.f && slab + 2 < mine) ask(slab + 2);
             }
         }
+        if (p.beta != 0.f) { // (after a failure: values asked for and not waited for)
+            const long long began = clock64();
+            for (; w.s != l.s || w.parity != l.parity; w.next())
+                while (!mbar_try(old + 8 * (2 * warp + w.s), w.parity) && clock64() - began < kMxWaitClocks) {}
+        }
+        if (by_tma && lane == 0) tma_stores_done();
+        __syncwarp();
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     __syncthreads();
