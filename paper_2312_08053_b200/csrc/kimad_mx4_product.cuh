@@ -339,7 +339,8 @@ k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
 // One CTA per SM stays for all its tiles; the sums are held twice, so that one tile's outputs are written beside the next one's products.  Outputs
 // on 16 bytes come and go by TMA, slab by slab: the stores of eight warps are more than an SM gets rid of at once (about 16 bytes per clock when all
 // write), and what waits in line behind them are the other warps' barriers, scales and products (stages took 2000 clocks beside them, 480 otherwise).
-// Warps: 0-7 outputs (a quarter of the lines and half of the columns each), 8-11 scales, 12 copies, 13 products (in the pair's first CTA).
+// Warps: 0-7 outputs (a quarter of the lines and half of the columns each), 8-11 scales to tensor memory, 12 copies of codes, 14 of scales (a copy takes
+// almost 100 clocks to issue; all five of a stage in one warp are more than its products take), 13 products (in the pair's first CTA).
 constexpr uint32_t kMxPairN = 192;
 constexpr uint32_t kMxPairStages = 5;
 constexpr uint32_t kMxPairBytesB = kMxPairN / 2 * 128;
@@ -347,7 +348,7 @@ constexpr uint32_t kMxPairScales = 2 * 512; // bytes of a stage's scales of a ti
 constexpr uint32_t kMxPairStageBytes = kMxOperandStage + kMxPairBytesB + 3 * kMxPairScales;
 constexpr uint32_t kMxPairOut = 2 * 4096; // bytes of a warp's outputs: two slabs of 32 by 32, or one of 32 by 33
 constexpr uint32_t kMxPairSmem = 1024 + kMxPairStages * kMxPairStageBytes + 8 * kMxPairOut;
-constexpr int kMxPairThreads = 448;
+constexpr int kMxPairThreads = 480;
 constexpr uint32_t kMxPairScaleCols = 24; // of a stage: A's 2 x 4, B's 2 x 8 (6 in use)
 static_assert(2 * kMxPairN + kMxPairStages * kMxPairScaleCols <= 512, "tensor memory");
 static_assert(kMxPairSmem <= 227 * 1024 && kMxPairStageBytes % 1024 == 0 && kMxPairN == 192, "shared memory; tc_store_scales");
@@ -415,7 +416,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         if (by_tma) tma_prefetch(&map_out);
     }
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 1); mbar_init(ready + 8 * s, 8); mbar_init(empty + 8 * s, 1); }
+        for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 2); mbar_init(ready + 8 * s, 8); mbar_init(empty + 8 * s, 1); }
         for (uint32_t b = 0; b < 2; ++b) { mbar_init(done + 8 * b, 1); mbar_init(drained + 8 * b, 16); }
         mbar_init(quit, 1);
         for (uint32_t i = 0; i < 16; ++i) mbar_init(old + 8 * i, 1);
@@ -440,21 +441,32 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (warp == 12) {
         for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
             const MxPairTile t(p, tile);
+            for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
+                const uint32_t to = smem + q.s * kMxPairStageBytes, here = full + 8 * q.s;
+                if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
+                if (one_lane()) {
+                    mbar_expect(here, kMxOperandStage + kMxPairBytesB);
+                    tma_load_3d(to, &map_a, (int)(r * 128), (int)(t.row + rank * kMxTile), (int)t.n, here);
+                    tma_load_3d(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(t.col + rank * (kMxPairN / 2)), (int)t.n, here);
+                }
+            }
+        }
+    } else if (warp == 14) {
+        for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
+            const MxPairTile t(p, tile);
             const uint32_t la = t.row / kMxTile + rank, lb = t.col / kMxTile; // tiles of lines whose scales are read
             const bool have_a = la < p.a.line_tiles, have_b = lb + 1 < p.b.line_tiles;
             const uint8_t* sa = p.scales_a + ((uint64_t)t.n * p.a.line_tiles + la) * tiles * 512;
             const uint8_t* sb = p.scales_b + ((uint64_t)t.n * p.b.line_tiles + lb) * tiles * 512;
             for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
-                const uint32_t to = smem + q.s * kMxPairStageBytes, here = full + 8 * q.s, scales = to + kMxOperandStage + kMxPairBytesB;
+                const uint32_t to = smem + q.s * kMxPairStageBytes + kMxOperandStage + kMxPairBytesB, here = full + 8 * q.s;
                 if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
                 if (one_lane()) {
                     const uint32_t bytes = min(tiles - 2 * r, 2u) * 512u;
-                    mbar_expect(here, kMxOperandStage + kMxPairBytesB + bytes * (1u + have_a + have_b));
-                    if (have_a) bulk_load(scales, sa + (uint64_t)r * 1024, bytes, here);
-                    bulk_load(scales + kMxPairScales, sb + (uint64_t)r * 1024, bytes, here);
-                    if (have_b) bulk_load(scales + 2 * kMxPairScales, sb + (uint64_t)tiles * 512 + (uint64_t)r * 1024, bytes, here);
-                    tma_load_3d(to, &map_a, (int)(r * 128), (int)(t.row + rank * kMxTile), (int)t.n, here);
-                    tma_load_3d(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(t.col + rank * (kMxPairN / 2)), (int)t.n, here);
+                    mbar_expect(here, bytes * (1u + have_a + have_b));
+                    if (have_a) bulk_load(to, sa + (uint64_t)r * 1024, bytes, here);
+                    bulk_load(to + kMxPairScales, sb + (uint64_t)r * 1024, bytes, here);
+                    if (have_b) bulk_load(to + 2 * kMxPairScales, sb + (uint64_t)tiles * 512 + (uint64_t)r * 1024, bytes, here);
                 }
             }
         }
