@@ -1146,7 +1146,7 @@ int mx4_prepare_product() {
     CUDA_TRY(cudaGetDevice(&dev));
     const uint64_t bit = 1ull << (dev & 63);
     if (dev >= 256 || !(raised[dev / 64].load(std::memory_order_acquire) & bit)) {
-        CUDA_TRY(cudaFuncSetAttribute(k_mx4_product, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxProductSmem));
+        CUDA_TRY(cudaFuncSetAttribute(k_mx4_product_parts, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxPartSmem));
         CUDA_TRY(cudaFuncSetAttribute(k_mx4_product_pairs, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxPairSmem));
         if (dev < 256) raised[dev / 64].fetch_or(bit, std::memory_order_release);
     }
@@ -1305,21 +1305,23 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
                       alpha, beta, status_dev};
     const uint64_t tiles = (uint64_t)p.a.line_tiles * p.b.line_tiles;
     if (tiles > 0x7fffffffull || batch > 0x7fffffffull / tiles) return KIMAD_ERR_INVALID_ARG;
-    const uint64_t pair_tiles = (m + 255) / 256 * ((n + kMxPairN - 1) / kMxPairN) * batch;
-    const bool pairs = length && pair_tiles >= 74;
-    CUtensorMap map_a{}, map_b{}; // (not looked at where nothing is summed)
+    const uint64_t pair_tiles = (m + 255) / 256 * ((n + kMxPairN - 1) / kMxPairN) * batch, all = tiles * batch, rounds = (p.a.blocks + 7) / 8;
+    // Parts of the summed axis.  Joining two or four costs about as much as eight rounds of products do, and is of use only while there are SMs for the parts:
+    // 256 x 2048 outputs (32 tiles) over 8192 values take 12.9 us by pairs, 9.7 by two parts, 10.2 by four; 512 x 512 (16 tiles) 13.2 / 10.3 / 9.3, over 2048 values
+    // 7.8 / 7.9 / 8.0; 1024 x 1024 (64 tiles) over 2048 7.9 / 9.1.
+    const uint32_t parts = rounds < 12 ? 1u : all <= 18 ? 4u : all <= 74 && rounds >= 16 ? 2u : 1u;
+    const bool pairs = length && parts == 1;
+    CUtensorMap map_a{}, map_b{}, map_out{}; // (not looked at where nothing is summed)
     if (length && (!mx4_map(&map_a, a_codes_dev, p.a, batch, kMxTile) || !mx4_map(&map_b, b_codes_dev, p.b, batch, pairs ? kMxPairN / 2 : kMxTile)))
         return KIMAD_ERR_CUDA;
     { const int rc = mx4_prepare_product(); if (rc != KIMAD_OK) return rc; }
     if (pairs) {
-        CUtensorMap map_out{};
         const uint32_t by_tma = mx4_map_output(&map_out, out_dev, m, n, batch, ld, batch_stride);
         CUDA_TRY(launch_pdl(k_mx4_product_pairs, dim3((uint32_t)std::min<uint64_t>(pair_tiles, 74) * 2), kMxPairThreads, kMxPairSmem, s, map_a, map_b,
                             map_out, p, (uint32_t)pair_tiles, by_tma));
-        CUDA_TRY(cudaGetLastError());
-        return KIMAD_OK;
+    } else {
+        CUDA_TRY(launch_clusters("k_mx4_product_parts", parts, k_mx4_product_parts, dim3((uint32_t)all, 1, parts), kMxPartThreads, kMxPartSmem, s, map_a, map_b, p));
     }
-    CUDA_TRY(launch_pdl(k_mx4_product, dim3((uint32_t)(tiles * batch)), kMxProductThreads, kMxProductSmem, s, map_a, map_b, p));
     CUDA_TRY(cudaGetLastError());
     return KIMAD_OK;
 }

@@ -5,12 +5,10 @@
 // scales' tiles (128 lines by 4 blocks, 512 bytes) are in the order that tensor memory wants: lane r % 32 (in all four quarters of it), column
 // r / 32, a byte per block.
 //
-// A CTA makes a tile of 128 by 128 outputs: one warp brings stages of 256 values (128 bytes) of 128 lines of either operand by TMA, 128-byte
-// swizzled, and their scales by bulk copies; four warps store the scales to tensor memory, a quarter each; one thread of another warp issues the
-// products.  (Copies of the scales by tcgen05.cp wait in line with the products: a stage then took 590 clocks of an SM, 256 of them products.)
-// The four warps then take the sums out (32 lines each), turn slabs of 32 by 32 around in shared memory and update the output in lines of
-// consecutive elements, whatever its alignment; the first of the output's old values are under way while the products run.  Two CTAs share
-// an SM: one's outputs are written beside the other's products.
+// One warp brings stages of 256 values (128 bytes) of the operands' lines by TMA, 128-byte swizzled; four warps bring the scales to tensor memory, a
+// quarter each (copies by tcgen05.cp wait in line with the products: a stage of 128 by 128 then took 590 clocks of an SM, 256 of them products); one
+// lane of another warp issues the products; further warps take the sums out and update the output.
+// k_mx4_product_pairs has two SMs for a tile, k_mx4_product_parts several for parts of the summed axis of one.
 // Lines behind the operand's last and bytes behind a line's last block are filled with zeros by TMA: code 0 times any scale that is there
 // is 0, and the scales that are not there are 0 too.
 // Waits are bounded (kMxWaitClocks): a CTA whose wait ran out stores nothing, waits for its copies, frees its tensor memory and sets the status.
@@ -21,13 +19,8 @@
 
 namespace kimad {
 
-constexpr int kMxStages = 3;
 constexpr uint32_t kMxStageK = 256;                  // values of the summed axis in a stage
 constexpr uint32_t kMxOperandStage = 128 * 128;      // bytes of codes of an operand in a stage
-constexpr uint32_t kMxStageBytes = 2 * kMxOperandStage;
-constexpr uint32_t kMxProductSmem = 1024 + kMxStages * kMxStageBytes;
-constexpr int kMxProductThreads = 192;               // warps 0-3 scales and outputs, 4 copies, 5 products
-constexpr uint32_t kMxTmemCols = 256;                // 128 of sums, 16 of scales a stage
 constexpr long long kMxWaitClocks = 1ll << 31;       // about a second
 
 // Instruction descriptor of kind mxf4: E2M1 by E2M1, scales UE8M0, K-major, N (bits 17-22, in eights), M (bits 27-28, in 128s).
@@ -150,10 +143,19 @@ struct MxOutput {
         aligned = reinterpret_cast<uintptr_t>(at) % 32 == 0 && ld % 8 == 0;
     }
     __device__ __forceinline__ bool whole(uint32_t slab) const { return aligned && 32 * slab + 32 <= cols; }
+    // A slab's old values: a lane's row where it is whole, otherwise a lane's column.
     __device__ __forceinline__ void fetch(uint32_t slab, float (&was)[32]) const {
-        if (beta != 0.f && whole(slab) && lane < rows) {
+        if (beta == 0.f) return;
+        if (whole(slab)) {
+            if (lane < rows) {
 #pragma unroll
-            for (uint32_t i = 0; i < 32; i += 8) mx_load8(mine + 32 * slab + i, *reinterpret_cast<float(*)[8]>(&was[i]));
+                for (uint32_t i = 0; i < 32; i += 8) mx_load8(mine + 32 * slab + i, *reinterpret_cast<float(*)[8]>(&was[i]));
+            }
+        } else {
+            const float* from = at + 32 * slab + lane;
+            const uint32_t here = 32 * slab + lane < cols ? rows : 0u;
+#pragma unroll
+            for (uint32_t i = 0; i < 32; ++i, from += ld) was[i] = i < here ? __ldcs(from) : 0.f;
         }
     }
     __device__ __forceinline__ float update(uint32_t sum, float was) const {
@@ -173,85 +175,143 @@ struct MxOutput {
             }
             return;
         }
-        put_any(slab, sums, buf);
-    }
-    __device__ __forceinline__ void put_any(uint32_t slab, const uint32_t (&sums)[32], float* buf) const {
         if (32 * slab >= cols || rows == 0) return;
         __syncwarp();
 #pragma unroll
         for (uint32_t i = 0; i < 32; ++i) buf[lane * 33 + i] = __uint_as_float(sums[i]);
         __syncwarp();
-        const bool in = 32 * slab + lane < cols;
+        float x[32]; // all of them before the first store: the compiler cannot tell that the output is not in shared memory
+#pragma unroll
+        for (uint32_t i = 0; i < 32; ++i) x[i] = buf[i * 33 + lane];
         float* to = at + 32 * slab + lane;
-#pragma unroll 1
-        for (uint32_t i0 = 0; i0 < rows; i0 += 8, to += 8 * ld) { // eight rows' loads before their stores: the compiler cannot tell that they are not the same place
-            float x[8], old[8];
+        const uint32_t here = 32 * slab + lane < cols ? rows : 0u;
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-                x[i] = buf[(i0 + i) * 33 + lane];
-                old[i] = beta != 0.f && in && i0 + i < rows ? to[i * ld] : 0.f;
-            }
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i)
-                if (in && i0 + i < rows) to[i * ld] = update(__float_as_uint(x[i]), old[i]);
-        }
+        for (uint32_t i = 0; i < 32; ++i, to += ld)
+            if (i < here) asm volatile("st.global.f32 [%0], %1;" ::"l"(to), "f"(update(__float_as_uint(x[i]), was[i])) : "memory");
     }
 };
 
 // The scales of two blocks of four for this lane's quarter: a line of each 32, 16 bytes.  0 where there are none.
-__device__ __forceinline__ uint4 mx_scale_words(const uint8_t* tile, uint32_t chunk, uint32_t chunks, bool have, uint32_t lane) {
-    return have && chunk < chunks ? __ldg(reinterpret_cast<const uint4*>(tile + (uint64_t)chunk * 512) + lane) : make_uint4(0, 0, 0, 0);
+__device__ __forceinline__ uint4 mx_scale_words(const uint8_t* tile, uint32_t chunk, uint32_t chunks, uint32_t lane) {
+    return chunk < chunks ? __ldg(reinterpret_cast<const uint4*>(tile + (uint64_t)chunk * 512) + lane) : make_uint4(0, 0, 0, 0);
 }
 
-__global__ void __launch_bounds__(kMxProductThreads, 2)
-k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MxProduct p) {
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint4 shared4(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 shared2(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
+// ... and of another CTA of the cluster.
+__device__ __forceinline__ uint32_t shared_of(uint32_t at, uint32_t rank) {
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    return there;
+}
+// A copy from here to there, counted on the barrier there.
+__device__ __forceinline__ void far_copy(uint32_t there, uint32_t src, uint32_t bytes, uint32_t bar_there) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(there), "r"(src), "r"(bytes), "r"(bar_there) : "memory");
+}
+__device__ __forceinline__ uint32_t mx_add(uint32_t a, uint32_t b) { return __float_as_uint(__fadd_rn(__uint_as_float(a), __uint_as_float(b))); }
+
+// ---- Parts.  Where there are few tiles and a long sum, a cluster of two or four CTAs shares a tile of 128 by 128 (gridDim.z of them): each takes a part of the
+// summed axis, copies its sums of a part of the tile's columns to each of the others' shared memory, and adds up those of its own part, in the order of the
+// CTAs.  (Also where nothing is summed at all.)  256 x 2048 outputs over 8192 values: 9.7 us with two
+// CTAs a tile, 12.9 by pairs of SMs.  With the sums read from the others' memory instead of copied there by the copy engine it took 13.5, with plain stores
+// to it 11.4.
+constexpr int kMxPartStages = 5;
+constexpr uint32_t kMxPartStageBytes = 2 * kMxOperandStage;
+constexpr uint32_t kMxJoin = 4 * 4 * 4096; // bytes of a tile's sums
+constexpr uint32_t kMxPartSmem = 1024 + kMxPartStages * kMxPartStageBytes + kMxJoin;
+constexpr int kMxPartThreads = 192;    // warps 0-3 scales and outputs, 4 copies, 5 products
+constexpr uint32_t kMxPartCols = 256;  // of tensor memory: 128 of sums, 16 of scales a stage
+static_assert(kMxPartSmem <= 227 * 1024 && 128 + 16 * kMxPartStages <= kMxPartCols, "memory");
+
+template <uint32_t PARTS> __device__ __forceinline__ void mx_join(uint32_t slab, uint32_t lane, uint32_t (&sums)[32]) {
+#pragma unroll
+    for (uint32_t c = 0; c < 8; ++c) {
+        uint4 v[PARTS];
+#pragma unroll
+        for (uint32_t z = 0; z < PARTS; ++z) v[z] = shared4(slab + 4096 * z * (4 / PARTS) + ((c ^ (lane & 7u)) << 4));
+#pragma unroll
+        for (uint32_t z = 1; z < PARTS; ++z)
+            v[0] = make_uint4(mx_add(v[0].x, v[z].x), mx_add(v[0].y, v[z].y), mx_add(v[0].z, v[z].z), mx_add(v[0].w, v[z].w));
+        sums[4 * c] = v[0].x;
+        sums[4 * c + 1] = v[0].y;
+        sums[4 * c + 2] = v[0].z;
+        sums[4 * c + 3] = v[0].w;
+    }
+}
+
+__global__ void __launch_bounds__(kMxPartThreads, 1)
+k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MxProduct p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t s_bar[3 * kMxStages + 1];
+    constexpr uint32_t S = kMxPartStages;
+    __shared__ __align__(8) uint64_t s_bar[3 * S + 2];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
     const uint32_t warp = warp_number(), lane = threadIdx.x & 31;
-    const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t full = bar, empty = bar + 8 * kMxStages, scaled = bar + 16 * kMxStages, done = bar + 24 * kMxStages; // a stage's copies, products, scales; all products
-    if (warp == 4 && lane == 0 && p.a.blocks) { tma_prefetch(&map_a); tma_prefetch(&map_b); }
+    const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u, parts = gridDim.z, part = blockIdx.z;
+    const uint32_t full = bar, empty = bar + 8 * S, scaled = bar + 16 * S, done = bar + 24 * S, joined = done + 8; // a stage's copies, products, scales; all products; all parts' sums
+    if (warp == 4 && p.a.blocks && one_lane()) { tma_prefetch(&map_a); tma_prefetch(&map_b); }
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < kMxStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); mbar_init(scaled + 8 * s, 4); }
+        for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); mbar_init(scaled + 8 * s, 4); }
         mbar_init(done, 1);
+        mbar_init(joined, 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (parts > 1) mbar_expect(joined, kMxJoin);
     }
     if (warp == 5) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kMxTmemCols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kMxPartCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); // (waited for before anything is sent to another CTA)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     pdl_wait();
 
     const uint32_t bt = blockIdx.x % p.b.line_tiles, at = blockIdx.x / p.b.line_tiles % p.a.line_tiles;
     const uint32_t n = blockIdx.x / p.b.line_tiles / p.a.line_tiles;
-    const uint32_t rounds = (p.a.blocks + kMxStageK / kMxBlock - 1) / (kMxStageK / kMxBlock), tiles = p.a.block_tiles;
+    const uint32_t all_rounds = (p.a.blocks + kMxStageK / kMxBlock - 1) / (kMxStageK / kMxBlock), tiles = p.a.block_tiles;
+    const uint32_t most = (all_rounds + parts - 1) / parts, first = min(part * most, all_rounds), rounds = min(all_rounds - first, most); // of this CTA
     uint32_t r = 0; // rounds whose copies, or whose products, have been issued
+    float was[2][32];
+    const MxOutput o(p, n, at * kMxTile + warp * 32, bt * kMxTile, kMxTile, lane); // (of warps 0-3)
+    const uint32_t mine = tmem + (warp * 32 << 16);
+    bool fine = false;
+    MxRing<S> q;
     if (warp == 4) {
-        MxRing<kMxStages> q;
         for (; r < rounds; ++r, q.next()) {
-            const uint32_t to = smem + q.s * kMxStageBytes, ready = full + 8 * q.s;
-            if (r >= kMxStages && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
+            const uint32_t to = smem + q.s * kMxPartStageBytes, ready = full + 8 * q.s;
+            if (r >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
             if (one_lane()) {
-                mbar_expect(ready, kMxStageBytes);
-                tma_load_3d(to, &map_a, (int)(r * 128), (int)(at * kMxTile), (int)n, ready);
-                tma_load_3d(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(bt * kMxTile), (int)n, ready);
+                mbar_expect(ready, kMxPartStageBytes);
+                tma_load_3d(to, &map_a, (int)((first + r) * 128), (int)(at * kMxTile), (int)n, ready);
+                tma_load_3d(to + kMxOperandStage, &map_b, (int)((first + r) * 128), (int)(bt * kMxTile), (int)n, ready);
             }
         }
     } else if (warp == 5) {
-        MxRing<kMxStages> q;
         for (; r < rounds; ++r, q.next()) {
             const uint32_t scales = tmem + kMxTile + 16 * q.s;
-            const uint64_t a = mx_desc_codes(smem + q.s * kMxStageBytes), b = mx_desc_codes(smem + q.s * kMxStageBytes + kMxOperandStage);
+            const uint64_t a = mx_desc_codes(smem + q.s * kMxPartStageBytes), b = mx_desc_codes(smem + q.s * kMxPartStageBytes + kMxOperandStage);
             if (!mbar_wait(scaled + 8 * q.s, q.parity, &s_failed)) break; // ... which the warps that stored them have waited for `full` with
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t products = min((p.a.blocks - r * 8 + 1) / 2, 4u); // of 64 values, two blocks, each
+            const uint32_t products = min((p.a.blocks - (first + r) * 8 + 1) / 2, 4u); // of 64 values, two blocks, each
             if (one_lane()) {
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k)
@@ -260,25 +320,16 @@ k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             }
         }
         if (one_lane()) tc_commit<1>(done);
-    }
-    __syncwarp();
-    if (warp < 4) {
-        const MxOutput o(p, n, at * kMxTile + warp * 32, bt * kMxTile, kMxTile, lane);
-        float* buf = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw))) + warp * 32 * 33;
+    } else {
         const uint8_t* sa = p.scales_a + ((uint64_t)n * p.a.line_tiles + at) * tiles * 512;
         const uint8_t* sb = p.scales_b + ((uint64_t)n * p.b.line_tiles + bt) * tiles * 512;
-        const uint32_t mine = tmem + (warp * 32 << 16);
-        float was[2][32];
-        o.fetch(0, was[0]);
-        o.fetch(1, was[1]);
-        auto load = [&](uint32_t r, uint4 (&v)[4]) {
+        auto load = [&](uint32_t i, uint4 (&v)[4]) {
 #pragma unroll
             for (uint32_t k = 0; k < 2; ++k) {
-                v[k] = mx_scale_words(sa, 2 * r + k, tiles, true, lane);
-                v[2 + k] = mx_scale_words(sb, 2 * r + k, tiles, true, lane);
+                v[k] = mx_scale_words(sa, 2 * (first + i) + k, tiles, lane);
+                v[2 + k] = mx_scale_words(sb, 2 * (first + i) + k, tiles, lane);
             }
         };
-        MxRing<kMxStages> q;
         auto store = [&](const uint4 (&v)[4]) {
             if (!mbar_wait(full + 8 * q.s, q.parity, &s_failed)) return false; // (and so the products that used the scales' place before are done)
             __syncwarp();
@@ -292,48 +343,77 @@ k_mx4_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         uint4 v0[4], v1[4]; // two rounds under way
         load(0, v0);
         load(1, v1);
-        for (uint32_t r = 0; r < rounds; r += 2) {
+        o.fetch(part, was[0]); // behind the scales, which the products wait for
+        if (part + parts < 4) o.fetch(part + parts, was[1]);
+        for (uint32_t i = 0; i < rounds; i += 2) {
             if (!store(v0)) break;
-            load(r + 2, v0);
-            if (r + 1 >= rounds || !store(v1)) break;
-            load(r + 3, v1);
+            load(i + 2, v0);
+            if (i + 1 >= rounds || !store(v1)) break;
+            load(i + 3, v1);
         }
-        const bool fine = mbar_wait(done, 0, &s_failed) && !s_failed;
+        fine = mbar_wait(done, 0, &s_failed) && !s_failed;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (fine) {
-#pragma unroll
-            for (uint32_t slab = 0; slab < 4; ++slab) {
-                uint32_t sums[32];
-                if (rounds) tc_load32(sums, mine + 32 * slab);
-                else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) sums[i] = 0;
-                }
-                o.put(slab, sums, was[slab & 1], buf);
-                if (slab < 2) o.fetch(slab + 2, was[slab & 1]);
-            }
-        }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    // Sums that the CTAs exchange: slabs of 32 by 32, a warp's four behind each other (CTA 0's for this one, CTA 1's, ..), sixteen bytes c of row i at c ^ (i % 8).
+    // They leave from where the stages were.
+    const uint32_t in = smem + S * kMxPartStageBytes + warp * 4 * 4096, out = smem + warp * 4 * 4096;
+    float* buf = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + kMxJoin) + warp * 32 * 33;
+    if (warp < 4 && fine && parts > 1) {
+#pragma unroll 1
+        for (uint32_t slab = 0; slab < 4; ++slab) {
+            uint32_t sums[32];
+            if (rounds) tc_load32(sums, mine + 32 * slab);
+#pragma unroll
+            for (uint32_t c = 0; c < 8; ++c)
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(out + 4096 * slab + lane * 128 + ((c ^ (lane & 7u)) << 4)), "r"(rounds ? sums[4 * c] : 0u),
+                             "r"(rounds ? sums[4 * c + 1] : 0u), "r"(rounds ? sums[4 * c + 2] : 0u), "r"(rounds ? sums[4 * c + 3] : 0u) : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (one_lane())
+                far_copy(shared_of(in + 4096 * (part * (4 / parts) + slab / parts), slab % parts), out + 4096 * slab, 4096, shared_of(joined, slab % parts));
+        }
+        fine = mbar_wait(joined, 0, &s_failed);
+        __syncwarp();
+    }
+    if (warp < 4 && fine) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t slab = part + i * parts;
+            if (slab >= 4) break;
+            uint32_t sums[32];
+            if (parts == 4) mx_join<4>(in + 4096 * i + lane * 128, lane, sums);
+            else if (parts == 2) mx_join<2>(in + 4096 * i + lane * 128, lane, sums);
+            else if (rounds) tc_load32(sums, mine + 32 * slab);
+            else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) sums[k] = 0;
+            }
+            o.put(slab, sums, was[i & 1], buf);
+            if (i < 2 && slab + 2 * parts < 4) o.fetch(slab + 2 * parts, was[i & 1]);
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (s_failed) { // what was issued still writes to this CTA's shared and tensor memory
         if (threadIdx.x == 0 && p.status) *p.status = KIMAD_ERR_TIMEOUT;
         const long long began = clock64();
         if (warp == 4 && lane == 0)
-            for (uint32_t i = r > kMxStages ? r - kMxStages : 0; i < r; ++i)
-                while (!mbar_try(full + 8 * (i % kMxStages), (i / kMxStages) & 1u) && clock64() - began < kMxWaitClocks) {}
+            for (uint32_t i = r > S ? r - S : 0; i < r; ++i)
+                while (!mbar_try(full + 8 * (i % S), (i / S) & 1u) && clock64() - began < kMxWaitClocks) {}
         if (warp == 5 && lane == 0)
             while (!mbar_try(done, 0) && clock64() - began < kMxWaitClocks) {}
         __syncwarp();
     }
+    cluster_sync(); // the copies from this CTA's memory have arrived
     if (warp == 5) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kMxTmemCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kMxPartCols) : "memory");
     }
 }
 
-// ---- Pairs.  Where there are enough tiles, two CTAs (SMs) take tiles of 256 by kMxPairN together (cta_group::2): each holds 128 of A's lines and half of
+// ---- Pairs.  Two CTAs (SMs) take tiles of 256 by kMxPairN together (cta_group::2): each holds 128 of A's lines and half of
 // B's in shared memory, and both tensor cores read both halves.  An SM then reads 28 KB of codes per 256 values of a tile of 128 by 192 sums, where 128 by
 // 128 alone needs 32: an SM takes 64 bytes per clock from L2, so a tile alone runs at half the products' rate at most.
 // One CTA per SM stays for all its tiles; the sums are held twice, so that one tile's outputs are written beside the next one's products.  Outputs
@@ -353,28 +433,10 @@ constexpr uint32_t kMxPairScaleCols = 24; // of a stage: A's 2 x 4, B's 2 x 8 (6
 static_assert(2 * kMxPairN + kMxPairStages * kMxPairScaleCols <= 512, "tensor memory");
 static_assert(kMxPairSmem <= 227 * 1024 && kMxPairStageBytes % 1024 == 0 && kMxPairN == 192, "shared memory; tc_store_scales");
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 // Arrival on the barrier of the pair's first CTA.  Relaxed: what is handed over are accesses to tensor memory that have been waited for (tcgen05.wait) and
 // copies that have been, none of the thread's own writes; with release the arrival waits for every store under way, about 1000 clocks.
 __device__ __forceinline__ void mbar_arrive_first(uint32_t bar) {
     asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %0, 0;\nmbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [a];\n}" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ uint4 shared4(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-    return v;
-}
-__device__ __forceinline__ uint2 shared2(uint32_t at) {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
-    return v;
 }
 // A's eight words, and B's twelve at columns 8-13 and 16-21.
 __device__ __forceinline__ void tc_store_scales(uint32_t addr, const uint4 (&a)[2], const uint2 (&b)[6]) {
@@ -557,7 +619,11 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     __syncwarp();
                     if (one_lane()) mbar_arrive_first(drained + 8 * u.s);
                 }
-                if (!by_tma) o.put_any(slab, sums, buf);
+                if (!by_tma) {
+                    float was[32];
+                    o.fetch(slab, was);
+                    o.put(slab, sums, was, buf);
+                }
                 if (slab >= mine) continue;
                 // sixteen bytes c of row r lie at c ^ (r % 8): no two of eight lanes meet in a bank
                 const uint32_t at = slabs + 4096 * w.s + lane * 128;

@@ -46,6 +46,8 @@ def exact_matrix(shape, rng):
 
 SHAPES = [(1, 1, 1, 1), (1, 128, 128, 64), (1, 128, 128, 256), (1, 7, 300, 33), (1, 300, 7, 65), (2, 129, 127, 31), (3, 64, 257, 97), (1, 130, 131, 129),
           (1, 256, 384, 1000), (4, 20, 30, 511), (1, 1, 1000, 257), (2, 513, 1, 768), (1, 128, 128, 800),
+          # few tiles and a long sum: shared by two and by four CTAs, the last of which may be left with nothing
+          (1, 256, 200, 3073), (1, 130, 129, 4097), (2, 70, 60, 4351), (9, 200, 256, 4100), (1, 1, 1, 3329), (36, 128, 128, 4096),
           # enough tiles of 256 x 192 for pairs of SMs: whole and cut in every direction, more tiles than pairs, more rounds than stages
           (1, 2560, 1536, 64), (40, 130, 200, 300), (80, 20, 30, 511), (1, 2500, 2000, 33), (3, 1300, 1000, 1000), (19, 257, 193, 900), (76, 256, 192, 256)]
 
