@@ -279,7 +279,7 @@ int kimad_mx4_read(const kimad_ctx* ctx, const kimad_mx4_message* msg, void* out
  *   codes   u8 [batch][lines][16 ceil(length / 32)]                             16-byte aligned
  *   scales  u8 [batch][ceil(lines / 128)][ceil(length / 128)][512]              16-byte aligned; line r and block b of a tile (128 lines by
  *           4 blocks) at byte (r mod 32) 16 + (r div 32) 4 + b; 0 for lines and blocks that are not there
- * lines and length at most 2^30, tiles of a batch below 2^31.
+ * lines and length at most 2^30, tiles of a batch below 2^27.
  * kimad_mx4_operand_bytes: of one matrix of the batch.  Host-only.
  * kimad_mx4_quantize: x_dev [batch][rows][cols] of dtype, `ld` elements from row to row (ld >= cols) and batch_stride from matrix to matrix
  *   (0: the same one).  along 0: blocks run over the rows, the operand has `cols` lines of `rows` values (x is transposed: tokens by

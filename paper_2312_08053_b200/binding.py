@@ -453,16 +453,15 @@ def _mx4_dtype(t, what, most=KIMAD_F16):
     return code
 
 
-def _mx4_stream(what, stream, *tensors):
-    """The library takes memory of the current device: a tensor of another one is refused, as is one in host memory."""
-    for t in tensors:
-        if not t.is_cuda:
-            raise ValueError(f"{what}: tensor on {t.device}, not on the current CUDA device")
-    device = _mx4_device()
-    for t in tensors:
-        if t.get_device() != device:
-            raise ValueError(f"{what}: tensor on {t.device}, the current device is cuda:{device}")
-    return _mx4_raw_stream(device) if stream is None else _stream_ptr(stream)
+def _mx4_stream(what, stream, *devices):
+    """The library takes memory of the current device: a tensor of another one is refused, as is one in host memory (device -1)."""
+    if min(devices) < 0:
+        raise ValueError(f"{what}: a tensor in host memory")
+    here = _mx4_device()
+    for d in devices:
+        if d != here:
+            raise ValueError(f"{what}: a tensor on cuda:{d}, the current device is cuda:{here}")
+    return _mx4_raw_stream(here) if stream is None else _stream_ptr(stream)
 
 
 def _mx4_workers(ctx, t, what):
@@ -500,6 +499,7 @@ class Mx4Message:
         self.stats = torch.zeros((W, STATS_DTYPE.itemsize), dtype=torch.uint8, device=device)
         self.c = kimad_mx4_message(self.codes.data_ptr(), self.scales.data_ptr(), self.err.data_ptr(), self.stats.data_ptr())
         self.ref = C.byref(self.c)
+        self.device = self.codes.get_device()
 
     def stats_host(self) -> np.ndarray:
         return self.stats.cpu().numpy().view(STATS_DTYPE).reshape(-1)
@@ -518,8 +518,8 @@ def kimad_mx4_step(ctx: Ctx, grads, state, msg: Mx4Message, stream=None) -> None
     _mx4_workers(ctx, grads, "grads")
     _mx4_workers(ctx, state, "state")
     m = _mx4_message(ctx, msg, "kimad_mx4_step")
-    s = _mx4_stream("kimad_mx4_step", stream, grads, state, msg.codes)
-    _check(load().kimad_mx4_step(ctx.handle, grads.data_ptr(), dtype, state.data_ptr(), m, s), "kimad_mx4_step")
+    s = _mx4_stream("kimad_mx4_step", stream, grads.get_device(), state.get_device(), msg.device)
+    _check((_lib or load()).kimad_mx4_step(ctx.handle, grads.data_ptr(), dtype, state.data_ptr(), m, s), "kimad_mx4_step")
 
 
 def kimad_mx4_apply(ctx: Ctx, msg: Mx4Message, est, x=None, weights=None, gamma=0.0, stream=None) -> None:
@@ -528,15 +528,15 @@ def kimad_mx4_apply(ctx: Ctx, msg: Mx4Message, est, x=None, weights=None, gamma=
     _mx4_workers(ctx, est, "est")
     m = _mx4_message(ctx, msg, "kimad_mx4_apply")
     if x is None:
-        s = _mx4_stream("kimad_mx4_apply", stream, est, msg.codes)
-        _check(load().kimad_mx4_apply(ctx.handle, m, est.data_ptr(), None, None, 0.0, s), "kimad_mx4_apply")
+        s = _mx4_stream("kimad_mx4_apply", stream, est.get_device(), msg.device)
+        _check((_lib or load()).kimad_mx4_apply(ctx.handle, m, est.data_ptr(), None, None, 0.0, s), "kimad_mx4_apply")
         return
     _mx4_dtype(x, "x", KIMAD_F32)
     w = np.ascontiguousarray([] if weights is None else weights, dtype=np.float32).reshape(-1)
     if w.size != ctx.W or x.dim() != 1 or x.numel() != ctx.N or (ctx.N > 1 and x.stride(0) != 1):
         raise ValueError(f"kimad_mx4_apply: x of {ctx.N} consecutive elements and {ctx.W} weights")
-    s = _mx4_stream("kimad_mx4_apply", stream, est, x, msg.codes)
-    _check(load().kimad_mx4_apply(ctx.handle, m, est.data_ptr(), x.data_ptr(), w.ctypes.data_as(C.POINTER(C.c_float)), gamma, s), "kimad_mx4_apply")
+    s = _mx4_stream("kimad_mx4_apply", stream, est.get_device(), x.get_device(), msg.device)
+    _check((_lib or load()).kimad_mx4_apply(ctx.handle, m, est.data_ptr(), x.data_ptr(), w.ctypes.data_as(C.POINTER(C.c_float)), gamma, s), "kimad_mx4_apply")
 
 
 def kimad_mx4_read(ctx: Ctx, msg: Mx4Message, out, stream=None) -> None:
@@ -544,8 +544,8 @@ def kimad_mx4_read(ctx: Ctx, msg: Mx4Message, out, stream=None) -> None:
     dtype = _mx4_dtype(out, "out", KIMAD_BF16)
     _mx4_workers(ctx, out, "out")
     m = _mx4_message(ctx, msg, "kimad_mx4_read")
-    s = _mx4_stream("kimad_mx4_read", stream, out, msg.codes)
-    _check(load().kimad_mx4_read(ctx.handle, m, out.data_ptr(), dtype, s), "kimad_mx4_read")
+    s = _mx4_stream("kimad_mx4_read", stream, out.get_device(), msg.device)
+    _check((_lib or load()).kimad_mx4_read(ctx.handle, m, out.data_ptr(), dtype, s), "kimad_mx4_read")
 
 
 def kimad_mx4_operand_bytes(lines: int, length: int):
@@ -557,7 +557,7 @@ def kimad_mx4_operand_bytes(lines: int, length: int):
 
 class Mx4Operand:
     """``batch`` matrices of ``lines`` lines of ``length`` values, quantised along their lines (see kimad.h for the layout): new device buffers, or
-    those of a message that has arrived."""
+    those of a message that has arrived (tensors that stay where they are)."""
 
     def __init__(self, lines: int, length: int, batch: int = 1, codes=None, scales=None, device="cuda"):
         import torch
@@ -569,18 +569,21 @@ class Mx4Operand:
         for t, n in ((self.codes, code_bytes), (self.scales, scale_bytes)):
             if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != batch * n:
                 raise ValueError(f"an operand of {batch} x {lines} x {length} has {batch * n} contiguous bytes, not {tuple(t.shape)} of {t.dtype}")
+        if self.codes.get_device() != self.scales.get_device():
+            raise ValueError("an operand's codes and scales are on one device")
+        self.device = self.codes.get_device()
+        self.codes_ptr, self.scales_ptr = self.codes.data_ptr(), self.scales.data_ptr()
 
 
 def _mx4_matrix(t, batch, rows, cols, what):
     """(row stride, matrix stride) of a [rows][cols] or [batch][rows][cols] tensor."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 2:
-        shape, stride = (1, *shape), (0, *stride)
-    if tuple(shape) != (batch, rows, cols):
+    stride = t.stride()
+    shape = t.shape if len(stride) == 3 else (1, *t.shape)
+    if shape != (batch, rows, cols):
         raise ValueError(f"{what}: {tuple(t.shape)} does not go with an operand, {batch} x {rows} x {cols} does")
-    ld = stride[1] if rows > 1 else cols
-    if (cols > 1 and stride[2] != 1) or ld < cols:
-        raise ValueError(f"{what}: rows of consecutive elements that do not overlap, not strides {t.stride()}")
+    ld = stride[-2] if rows > 1 else cols
+    if (cols > 1 and stride[-1] != 1) or ld < cols:
+        raise ValueError(f"{what}: rows of consecutive elements that do not overlap, not strides {stride}")
     return ld, stride[0] if batch > 1 else 0
 
 
@@ -596,8 +599,8 @@ def kimad_mx4_quantize(x, op: Mx4Operand, along: int, stream=None) -> None:
     dtype = _mx4_dtype(x, "x")
     rows, cols = _mx4_along(op, along)
     ld, bs = _mx4_matrix(x, op.batch, rows, cols, "x")
-    s = _mx4_stream("kimad_mx4_quantize", stream, x, op.codes, op.scales)
-    _check(load().kimad_mx4_quantize(x.data_ptr(), dtype, rows, cols, ld, op.batch, bs, along, op.codes.data_ptr(), op.scales.data_ptr(), s),
+    s = _mx4_stream("kimad_mx4_quantize", stream, x.get_device(), op.device)
+    _check((_lib or load()).kimad_mx4_quantize(x.data_ptr(), dtype, rows, cols, ld, op.batch, bs, along, op.codes_ptr, op.scales_ptr, s),
            "kimad_mx4_quantize")
 
 
@@ -606,8 +609,8 @@ def kimad_mx4_dequantize(op: Mx4Operand, out, along: int, stream=None) -> None:
     dtype = _mx4_dtype(out, "out", KIMAD_BF16)
     rows, cols = _mx4_along(op, along)
     ld, bs = _mx4_matrix(out, op.batch, rows, cols, "out")
-    s = _mx4_stream("kimad_mx4_dequantize", stream, out, op.codes, op.scales)
-    _check(load().kimad_mx4_dequantize(op.codes.data_ptr(), op.scales.data_ptr(), out.data_ptr(), dtype, rows, cols, ld, op.batch, bs, along, s),
+    s = _mx4_stream("kimad_mx4_dequantize", stream, out.get_device(), op.device)
+    _check((_lib or load()).kimad_mx4_dequantize(op.codes_ptr, op.scales_ptr, out.data_ptr(), dtype, rows, cols, ld, op.batch, bs, along, s),
            "kimad_mx4_dequantize")
 
 
@@ -618,13 +621,13 @@ def kimad_mx4_product(a: Mx4Operand, b: Mx4Operand, out, alpha=1.0, beta=0.0, st
     if a.length != b.length or a.batch != b.batch:
         raise ValueError(f"kimad_mx4_product: operands of {a.batch} x {a.length} and of {b.batch} x {b.length}")
     ld, bs = _mx4_matrix(out, a.batch, a.lines, b.lines, "out")
-    s = _mx4_stream("kimad_mx4_product", stream, out, a.codes, a.scales, b.codes, b.scales)
+    s = _mx4_stream("kimad_mx4_product", stream, out.get_device(), a.device, b.device)
     if status is not None:
         if str(status.dtype) != "torch.int32" or status.numel() < 1:
             raise TypeError("kimad_mx4_product: status is an int32 tensor")
-        _mx4_stream("kimad_mx4_product", stream, status)
-    _check(load().kimad_mx4_product(out.data_ptr(), ld, bs, a.lines, b.lines, a.length, a.batch, a.codes.data_ptr(), a.scales.data_ptr(),
-                                    b.codes.data_ptr(), b.scales.data_ptr(), alpha, beta, None if status is None else status.data_ptr(), s), "kimad_mx4_product")
+        _mx4_stream("kimad_mx4_product", stream, status.get_device())
+    _check((_lib or load()).kimad_mx4_product(out.data_ptr(), ld, bs, a.lines, b.lines, a.length, a.batch, a.codes_ptr, a.scales_ptr,
+                                    b.codes_ptr, b.scales_ptr, alpha, beta, None if status is None else status.data_ptr(), s), "kimad_mx4_product")
 
 
 class Monitor:

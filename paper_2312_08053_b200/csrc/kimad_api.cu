@@ -1121,7 +1121,7 @@ constexpr uint64_t kMxMostLines = 1ull << 30;
 bool mx4_operand_ok(uint64_t lines, uint64_t length, uint64_t batch, const void* codes, const void* scales) {
     if (lines > kMxMostLines || length > kMxMostLines || (uintptr_t)codes % 16 || (uintptr_t)scales % 16) return false;
     const MxOperand op((uint32_t)lines, (uint32_t)length);
-    const uint64_t tiles = (uint64_t)op.line_tiles * op.block_tiles;
+    const uint64_t tiles = std::max<uint64_t>((uint64_t)op.line_tiles * op.block_tiles, MxRowCuts(op).ctas());
     return tiles <= 0x7fffffffull && (tiles == 0 || batch <= 0x7fffffffull / tiles);
 }
 
@@ -1259,8 +1259,8 @@ int kimad_mx4_quantize(const void* x_dev, uint32_t dtype, uint64_t rows, uint64_
         if (along == 0)
             return launch_named("k_mx4_quantize_cols", k_mx4_quantize_cols<T>, dim3((uint32_t)(batch * op.line_tiles * op.block_tiles)), kThreads, 0, s, x,
                                 ld, batch_stride, op, codes_dev, scales_dev);
-        return launch_named("k_mx4_quantize_rows", k_mx4_quantize_rows<T>, dim3((uint32_t)std::min<uint64_t>(batch * MxRowCuts(op).ctas(), 1u << 30)), kThreads, 0, s, x,
-                            ld, batch_stride, batch, op, codes_dev, scales_dev);
+        return launch_named("k_mx4_quantize_rows", k_mx4_quantize_rows<T>, dim3((uint32_t)(batch * MxRowCuts(op).ctas())), kThreads, 0, s, x,
+                            ld, batch_stride, op, codes_dev, scales_dev);
     };
     CUDA_TRY(dtype == KIMAD_F32 ? launch(static_cast<const float*>(x_dev))
              : dtype == KIMAD_BF16 ? launch(static_cast<const __nv_bfloat16*>(x_dev)) : launch(static_cast<const __half*>(x_dev)));
@@ -1283,8 +1283,8 @@ int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, vo
         if (along == 0)
             return launch_named("k_mx4_dequantize_cols", k_mx4_dequantize_cols<T>, dim3((uint32_t)(batch * op.line_tiles * op.block_tiles)), kThreads, 0, s, x,
                                 ld, batch_stride, op, codes_dev, scales_dev);
-        return launch_named("k_mx4_dequantize_rows", k_mx4_dequantize_rows<T>, dim3((uint32_t)std::min<uint64_t>(batch * MxRowCuts(op).ctas(), 1u << 30)), kThreads, 0, s, x,
-                            ld, batch_stride, batch, op, codes_dev, scales_dev);
+        return launch_named("k_mx4_dequantize_rows", k_mx4_dequantize_rows<T>, dim3((uint32_t)(batch * MxRowCuts(op).ctas())), kThreads, 0, s, x,
+                            ld, batch_stride, op, codes_dev, scales_dev);
     };
     CUDA_TRY(dtype == KIMAD_F32 ? launch(static_cast<float*>(x_dev)) : launch(static_cast<__nv_bfloat16*>(x_dev)));
     CUDA_TRY(cudaGetLastError());

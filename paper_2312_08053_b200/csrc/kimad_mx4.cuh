@@ -447,17 +447,27 @@ k_mx4_read(MxMessage msg, const Chunk* __restrict__ chunks, const LayerDesc* __r
     const uint32_t* words = msg.words(w, sp.first);
     const uint8_t* bytes = msg.bytes(w, sp.first);
     const bool aligned = mx_aligned8(o);
-#pragma unroll 2
-    for (uint32_t b = (piece * kMxWarps + warp) * kMxGroup; b < sp.blocks; b += pieces * kMxWarps * kMxGroup) {
-        const uint32_t e = b * kMxBlock, lim = min(sp.left - e, kMxGroupElems);
-        uint32_t word, byte;
-        float v[8];
-        mx_fetch(words + b * 4, bytes + b, sp.blocks - b, lane, word, byte);
-        mx_decode(word, byte, v);
-        if (aligned && lim == kMxGroupElems) mx_put<true>(o + e, lim, lane, v, 0u);
-        else {
-            mx_from_blocks<false>(v, s_buf[warp], lane);
-            mx_put<false>(o + e, lim, lane, v, 0u);
+    constexpr uint32_t U = 4; // groups under way
+    const uint32_t step = pieces * kMxWarps * kMxGroup;
+    for (uint32_t b0 = (piece * kMxWarps + warp) * kMxGroup; b0 < sp.blocks; b0 += U * step) {
+        uint32_t word[U], byte[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint32_t b = b0 + u * step;
+            mx_fetch(words + b * 4, bytes + b, b < sp.blocks ? sp.blocks - b : 0u, lane, word[u], byte[u]);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint32_t b = b0 + u * step, e = b * kMxBlock;
+            if (b >= sp.blocks) break;
+            const uint32_t lim = min(sp.left - e, kMxGroupElems);
+            float v[8];
+            mx_decode(word[u], byte[u], v);
+            if (aligned && lim == kMxGroupElems) mx_put<true>(o + e, lim, lane, v, 0u);
+            else {
+                mx_from_blocks<false>(v, s_buf[warp], lane);
+                mx_put<false>(o + e, lim, lane, v, 0u);
+            }
         }
     }
 }
@@ -492,32 +502,34 @@ static_assert(kMxWarps == 8, "a warp for each of eight lines");
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-k_mx4_quantize_rows(const T* __restrict__ x, uint64_t ld, uint64_t batch_stride, uint64_t batch, MxOperand op, uint8_t* __restrict__ codes,
-                    uint8_t* __restrict__ scales) {
+k_mx4_quantize_rows(const T* __restrict__ x, uint64_t ld, uint64_t batch_stride, MxOperand op, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     pdl_wait();
     __shared__ __align__(16) float s_buf[kMxWarps][kMxGroupElems];
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const MxRowCuts cuts(op);
-    for (uint64_t cta = blockIdx.x; cta < batch * cuts.ctas(); cta += gridDim.x) {
-        const uint64_t n = cta / cuts.ctas();
-        const uint32_t in = (uint32_t)(cta % cuts.ctas()), line = in / cuts.pieces * 8 + warp, group0 = in % cuts.pieces * kMxRowGroups;
-        const T* row = x + n * batch_stride + (uint64_t)min(line, op.lines - 1) * ld;
-        uint32_t* words = reinterpret_cast<uint32_t*>(codes) + (n * op.lines + line) * op.blocks * 4;
-        uint8_t* tiles = scales + n * op.scale_bytes();
-        const bool aligned = mx_aligned8(row);
-        for (uint32_t i = 0; i < kMxRowGroups && group0 + i < cuts.groups; ++i) {
-            const uint32_t b = (group0 + i) * kMxGroup, e = b * kMxBlock, lim = line < op.lines ? min(op.length - e, kMxGroupElems) : 0u, own = b + lane / 4;
-            float v[8];
-            uint32_t byte;
-            if (aligned && lim == kMxGroupElems) mx_get<true>(row + e, lim, lane, v);
-            else {
-                mx_get<false>(row + e, lim, lane, v);
-                mx_to_blocks<false>(v, s_buf[warp], lane);
-            }
-            const uint32_t word = mx_quantize8(v, byte);
-            if (line < op.lines && own < op.blocks) words[b * 4 + lane] = word;
-            if (lane % 4 == 0 && own < op.block_tiles * 4) tiles[op.scale_word(line, own / 4) * 4 + own % 4] = (uint8_t)byte;
-        }
+    const uint32_t piece = blockIdx.x % cuts.pieces, line = blockIdx.x / cuts.pieces % cuts.line_sets * 8 + warp;
+    const uint64_t n = blockIdx.x / cuts.pieces / cuts.line_sets;
+    const uint32_t b0 = piece * kMxRowGroups * kMxGroup, e0 = b0 * kMxBlock, left = line < op.lines ? op.length - e0 : 0u; // values of the line from e0 on
+    const T* row = x + n * batch_stride + (uint64_t)min(line, op.lines - 1) * ld + e0;
+    uint32_t* words = reinterpret_cast<uint32_t*>(codes) + ((n * op.lines + line) * op.blocks + b0) * 4;
+    uint8_t* tiles = scales + n * op.scale_bytes();
+    float v[kMxRowGroups][8]; // all under way at once
+    if (mx_aligned8(row) && left >= kMxRowGroups * kMxGroupElems) {
+#pragma unroll
+        for (uint32_t i = 0; i < kMxRowGroups; ++i) mx_get<true>(row + i * kMxGroupElems, kMxGroupElems, lane, v[i]);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < kMxRowGroups; ++i) mx_get<false>(row + i * kMxGroupElems, left > i * kMxGroupElems ? left - i * kMxGroupElems : 0u, lane, v[i]);
+#pragma unroll
+        for (uint32_t i = 0; i < kMxRowGroups; ++i) mx_to_blocks<false>(v[i], s_buf[warp], lane);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kMxRowGroups; ++i) {
+        const uint32_t own = b0 + i * kMxGroup + lane / 4;
+        uint32_t byte;
+        const uint32_t word = mx_quantize8(v[i], byte);
+        if (line < op.lines && own < op.blocks) words[i * 32 + lane] = word;
+        if (lane % 4 == 0 && own < op.block_tiles * 4) tiles[op.scale_word(line, own / 4) * 4 + own % 4] = (uint8_t)byte;
     }
 }
 
@@ -615,35 +627,40 @@ __device__ __forceinline__ float mx_operand_scale(uint32_t byte) { return byte =
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-k_mx4_dequantize_rows(T* __restrict__ x, uint64_t ld, uint64_t batch_stride, uint64_t batch, MxOperand op, const uint8_t* __restrict__ codes,
-                      const uint8_t* __restrict__ scales) {
+k_mx4_dequantize_rows(T* __restrict__ x, uint64_t ld, uint64_t batch_stride, MxOperand op, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales) {
     pdl_wait();
     __shared__ __align__(16) float s_buf[kMxWarps][kMxGroupElems];
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const MxRowCuts cuts(op);
-    for (uint64_t cta = blockIdx.x; cta < batch * cuts.ctas(); cta += gridDim.x) {
-        const uint64_t n = cta / cuts.ctas();
-        const uint32_t in = (uint32_t)(cta % cuts.ctas()), line = in / cuts.pieces * 8 + warp, group0 = in % cuts.pieces * kMxRowGroups;
-        if (line >= op.lines) continue;
-        T* row = x + n * batch_stride + (uint64_t)line * ld;
-        const uint32_t* words = reinterpret_cast<const uint32_t*>(codes) + (n * op.lines + line) * op.blocks * 4;
-        const uint8_t* tiles = scales + n * op.scale_bytes();
-        const bool aligned = mx_aligned8(row);
+    const uint32_t piece = blockIdx.x % cuts.pieces, line = blockIdx.x / cuts.pieces % cuts.line_sets * 8 + warp;
+    const uint64_t n = blockIdx.x / cuts.pieces / cuts.line_sets;
+    if (line >= op.lines) return;
+    const uint32_t b0 = piece * kMxRowGroups * kMxGroup, e0 = b0 * kMxBlock, left = op.length - e0;
+    T* row = x + n * batch_stride + (uint64_t)line * ld + e0;
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(codes) + ((n * op.lines + line) * op.blocks + b0) * 4;
+    const uint8_t* tiles = scales + n * op.scale_bytes();
+    const bool aligned = mx_aligned8(row);
+    uint32_t word[kMxRowGroups], byte[kMxRowGroups]; // all under way at once
 #pragma unroll
-        for (uint32_t i = 0; i < kMxRowGroups; ++i) {
-            if (group0 + i >= cuts.groups) break;
-            const uint32_t b = (group0 + i) * kMxGroup, e = b * kMxBlock, lim = min(op.length - e, kMxGroupElems), own = b + lane / 4;
-            const uint32_t word = own < op.blocks ? __ldcs(words + b * 4 + lane) : 0u;
-            const float scale = mx_operand_scale(own < op.blocks ? (uint32_t)tiles[op.scale_word(line, own / 4) * 4 + own % 4] : 0u);
-            float v[8];
-            mx_values8(word, v);
+    for (uint32_t i = 0; i < kMxRowGroups; ++i) {
+        const uint32_t own = b0 + i * kMxGroup + lane / 4;
+        word[i] = own < op.blocks ? __ldcs(words + i * 32 + lane) : 0u;
+        byte[i] = own < op.blocks ? (uint32_t)tiles[op.scale_word(line, own / 4) * 4 + own % 4] : 0u;
+    }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], scale);
-            if (aligned && lim == kMxGroupElems) mx_put<true>(row + e, lim, lane, v, 0u);
-            else {
-                mx_from_blocks<false>(v, s_buf[warp], lane);
-                mx_put<false>(row + e, lim, lane, v, 0u);
-            }
+    for (uint32_t i = 0; i < kMxRowGroups; ++i) {
+        const uint32_t e = i * kMxGroupElems;
+        if (e >= left) break;
+        const uint32_t lim = min(left - e, kMxGroupElems);
+        const float scale = mx_operand_scale(byte[i]);
+        float v[8];
+        mx_values8(word[i], v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], scale);
+        if (aligned && lim == kMxGroupElems) mx_put<true>(row + e, lim, lane, v, 0u);
+        else {
+            mx_from_blocks<false>(v, s_buf[warp], lane);
+            mx_put<false>(row + e, lim, lane, v, 0u);
         }
     }
 }
