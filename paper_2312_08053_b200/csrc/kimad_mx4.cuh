@@ -692,20 +692,27 @@ k_mx4_dequantize_cols(T* __restrict__ x, uint64_t ld, uint64_t batch_stride, MxO
     const float x1 = mx_operand_scale((s_scales[in_line % 32 * 4 + 4 + in_line / 32] >> (8 * q)) & 255u);
     T* to = x + n * batch_stride + (uint64_t)row0 * ld + line;
     const bool two = (lt + 1) * kMxTile <= op.lines && (bt + 1) * kMxTile <= op.length && ld % 2 == 0 && reinterpret_cast<uintptr_t>(to) % (2 * sizeof(T)) == 0;
+    if (two) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            float v0[8], v1[8];
+            mx_values8(w0[i], v0);
+            mx_values8(w1[i], v1);
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j, to += ld) mx_store2(to, __fmul_rn(v0[j], x0), __fmul_rn(v1[j], x1));
+        }
+        return;
+    }
+    const uint32_t rows = min(op.length - row0, kMxBlock), rows1 = line + 1 < op.lines ? rows : 0u;
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
         float v0[8], v1[8];
         mx_values8(w0[i], v0);
         mx_values8(w1[i], v1);
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            T* at = to + (8 * i + j) * ld;
-            const float lo = __fmul_rn(v0[j], x0), hi = __fmul_rn(v1[j], x1);
-            if (two) mx_store2(at, lo, hi);
-            else if (row0 + 8 * i + j < op.length) {
-                at[0] = mx_make<T>(lo);
-                if (line + 1 < op.lines) at[1] = mx_make<T>(hi);
-            }
+        for (uint32_t j = 0; j < 8; ++j, to += ld) {
+            if (8 * i + j < rows) to[0] = mx_make<T>(__fmul_rn(v0[j], x0));
+            if (8 * i + j < rows1) to[1] = mx_make<T>(__fmul_rn(v1[j], x1));
         }
     }
 }
