@@ -241,8 +241,8 @@ int kimad_aggregate(float* x_dev, const float* est_dev, uint64_t stride, uint32_
  *   codes   u8 [W][code_bytes], scales u8 [W][scale_bytes]  both 16-byte aligned
  *   err     f32 [W][L]  ||d_l - C(d_l)||^2, summed in binary64; may be NULL where the message is only read
  *   stats   [W]         used_bytes = 17 bytes per block, n_selected = N, budget_bytes = 0 (no budget is taken); may be NULL likewise
- * The same contexts as for TopK, of any policy, with their workspace attached; the ratio grid and D play no role.  Steps of either kind may
- * follow each other on the same estimators. */
+ * The same contexts as for TopK, of any policy (at most 65535 workers), with their workspace attached; the ratio grid and D play no role.
+ * Steps of either kind may follow each other on the same estimators. */
 enum { KIMAD_F32 = 0, KIMAD_BF16 = 1, KIMAD_F16 = 2 }; /* element types of the calls below */
 typedef struct {
     uint8_t* codes;
@@ -260,7 +260,7 @@ int kimad_mx4_message_bytes(const kimad_ctx* ctx, uint64_t* code_bytes, uint64_t
  * An absent block (d is Inf or NaN somewhere in it) sends nothing: the estimator keeps its 32 values, the layer's err and the worker's
  * total_err are Inf, and with check_finite the worker's status is KIMAD_ERR_NONFINITE (its other blocks are sent).  Asynchronous on
  * cuda_stream, capturable, no synchronisation; any alignment of the elements (same speed).  Uses the context's workspace: as with
- * kimad_step, calls on one context follow each other on one stream.  Errors: INVALID_ARG, WORKSPACE, CUDA. */
+ * kimad_step, calls on one context (replays of graphs that hold them among them) follow each other on one stream.  Errors: INVALID_ARG, WORKSPACE, CUDA. */
 int kimad_mx4_step(kimad_ctx* ctx, const void* grads_dev, uint32_t grad_dtype, float* state_dev, const kimad_mx4_message* out, void* cuda_stream);
 
 /* The receiving side: est_m <- fl32(est_m + C_m) for every worker m (absent blocks leave est_m as it is), so that a receiver's copy stays

@@ -1,5 +1,9 @@
 """4-bit messages and operands on the GPU against their definition in 64 bits.  Codes, scales, states and values are compared bit for bit; sums of
 squares within half a step of binary32 for the one rounding at the end, and as much again for the order of the binary64 sums."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -10,6 +14,7 @@ from tests import _mx4
 from tests._harness import Runner
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 LAYERS = {
     "one": [1],
@@ -76,6 +81,7 @@ class Case:
             assert np.allclose(float(st["total_err"][w]), float(total), rtol=2.0 ** -23)
             assert int(st["used_bytes"][w]) == 17 * blocks and int(st["n_selected"][w]) == self.N and int(st["budget_bytes"][w]) == 0
         assert np.array_equal(bits(self.state), new.view(np.uint32))
+        assert kb.kimad_debug_check(self.ctx)[1:] == (0, 0)
 
 
 @pytest.mark.parametrize("layers,W,pad,dtype,shift", [
@@ -234,6 +240,33 @@ def test_captured_and_on_another_stream():
         assert torch.equal(a, b)
 
 
+def test_offsets_beyond_32_bits():
+    """Three workers more than 2^30 elements apart: the last one starts behind 2^31 elements."""
+    layers = [33, 70000, 5]
+    N, stride = sum(layers), (1 << 30) + 4099
+    ctx = kb.new_context(layers, 3, [1.0], worker_stride=stride)
+    msg = kb.Mx4Message(ctx)
+    rng = np.random.default_rng(4)
+    g = rng.standard_normal((3, N)).astype(np.float32)
+    grads = torch.zeros(2 * stride + N, dtype=torch.bfloat16, device="cuda").as_strided((3, N), (stride, 1))
+    state = torch.zeros(2 * stride + N, device="cuda").as_strided((3, N), (stride, 1))
+    grads.copy_(torch.from_numpy(g))
+    kb.kimad_mx4_step(ctx, grads, state, msg)
+    torch.cuda.synchronize()
+    d = grads.float().cpu().numpy()
+    for w in range(3):
+        c, sc, v, _, _ = _mx4.message(d[w], layers)
+        assert np.array_equal(msg.codes[w].cpu().numpy(), c) and np.array_equal(msg.scales[w, :len(sc)].cpu().numpy(), sc)
+        assert np.array_equal(state[w].cpu().numpy().astype(np.float64), v)
+    first = state.clone()
+    x = torch.zeros(N, device="cuda")
+    kb.kimad_mx4_apply(ctx, msg, state, x, [1.0, 1.0, 1.0], 1.0)
+    kb.kimad_mx4_read(ctx, msg, grads)
+    torch.cuda.synchronize()
+    assert torch.equal(state, 2 * first) and torch.equal(grads.float(), first)
+    assert torch.equal(x, -(state[0] + state[1] + state[2]))
+
+
 # ----------------------------------------------------------------------------- operands
 def _guarded(n):
     """n bytes on the device between two walls."""
@@ -296,3 +329,15 @@ def test_empty_matrices():
         kb.kimad_mx4_quantize(x, op, 0)
         kb.kimad_mx4_dequantize(op, x, 0)
     torch.cuda.synchronize()
+
+
+def test_under_the_checked_build():
+    """The same tests with the library's index tests and canaries on (a process of its own: the library is chosen when it is loaded)."""
+    from paper_2312_08053_b200 import build as kbuild
+
+    if os.environ.get("KIMAD_CHECKED") == "1":
+        pytest.skip("this process runs the checked build")
+    kbuild.build(checked=True)
+    res = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "tests/test_gpu_mx4.py"], cwd=ROOT, env=dict(os.environ, KIMAD_CHECKED="1"),
+                         capture_output=True, text=True, timeout=900)
+    assert res.returncode == 0 and " passed" in res.stdout, res.stdout[-3000:] + res.stderr[-2000:]

@@ -1,4 +1,8 @@
 """The product of two operands in 4-bit blocks against the same sums in 64 bits."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -7,6 +11,7 @@ from paper_2312_08053_b200 import binding as kb
 from tests import _mx4
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def operand(m):
@@ -48,7 +53,8 @@ SHAPES = [(1, 1, 1, 1), (1, 128, 128, 64), (1, 128, 128, 256), (1, 7, 300, 33), 
           (1, 256, 384, 1000), (4, 20, 30, 511), (1, 1, 1000, 257), (2, 513, 1, 768), (1, 128, 128, 800),
           # few tiles and a long sum: shared by two and by four CTAs, the last of which may be left with nothing
           (1, 256, 200, 3073), (1, 130, 129, 4097), (2, 70, 60, 4351), (9, 200, 256, 4100), (1, 1, 1, 3329), (36, 128, 128, 4096),
-          # enough tiles of 256 x 192 for pairs of SMs: whole and cut in every direction, more tiles than pairs, more rounds than stages
+          # outputs on 16 bytes and smaller than a slab; cut tiles of 256 x 192, whole ones, more tiles than pairs of SMs, more rounds than stages
+          (3, 5, 8, 100), (1, 40, 36, 70), (2, 300, 12, 65), (2, 300, 200, 2000), (1, 520, 400, 1500),
           (1, 2560, 1536, 64), (40, 130, 200, 300), (80, 20, 30, 511), (1, 2500, 2000, 33), (3, 1300, 1000, 1000), (19, 257, 193, 900), (76, 256, 192, 256)]
 
 
@@ -192,3 +198,89 @@ def test_a_round_with_factors_and_messages():
     assert torch.equal(est, state)
     # every pass leaves at most a quarter of a value (cut at 6 of up to 8 scales) or half a unit of the block's scale: what is left shrinks
     assert all(q < p for p, q in zip(left, left[1:]))
+
+
+def test_offsets_beyond_32_bits():
+    """Matrices of a batch more than 2^31 elements apart, on 16 bytes (by TMA) and not."""
+    rng = np.random.default_rng(8)
+    a, va = operand(exact_matrix((3, 130, 70), rng))
+    b, vb = operand(exact_matrix((3, 200, 70), rng))
+    want = np.matmul(va, vb.transpose(0, 2, 1))
+    stride = (1 << 30) + 4096
+    flat = torch.zeros(2 * stride + 130 * 204 + 64, device="cuda")
+    for shift, ld in ((0, 200), (1, 203)):
+        out = flat.as_strided((3, 130, 200), (stride, ld, 1), shift)
+        out.copy_(torch.ones((), device="cuda").expand(3, 130, 200))
+        kb.kimad_mx4_product(a, b, out, alpha=1.0, beta=2.0)
+        assert np.array_equal(out.cpu().numpy().astype(np.float64), want + 2.0)
+    x = flat.as_strided((3, 70, 130), (stride, 131, 1), 5)
+    x.copy_(torch.randn((3, 70, 130), device="cuda"))
+    op, back = kb.Mx4Operand(130, 70, batch=3), torch.zeros((3, 70, 130), device="cuda")
+    kb.kimad_mx4_quantize(x, op, 0)
+    kb.kimad_mx4_dequantize(op, back, 0)
+    values = np.stack([_mx4.operand(np.ascontiguousarray(m.cpu().numpy().T))[2].T for m in x])
+    assert np.array_equal(back.cpu().numpy().astype(np.float64), values)
+    kb.kimad_mx4_dequantize(op, x, 0)
+    assert torch.equal(x, back)
+
+
+def test_two_at_once_on_streams_given_by_argument():
+    """Products by pairs and by parts beside each other, and each replayed from a graph of its own."""
+    rng = np.random.default_rng(9)
+    work = []
+    for m, n, length in ((700, 500, 300), (200, 130, 4500), (40, 36, 64)):
+        a, va = operand(exact_matrix((1, m, length), rng))
+        b, vb = operand(exact_matrix((1, n, length), rng))
+        work.append((a, b, va[0] @ vb[0].T if length <= 1100 else None, [torch.zeros((m, n), device="cuda") for _ in range(3)], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for a, b, _, out, s in work:
+        kb.kimad_mx4_product(a, b, out[0])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for a, b, _, out, s in work:
+            kb.kimad_mx4_product(a, b, out[1], stream=s)
+    torch.cuda.synchronize()
+    graphs = []
+    for a, b, _, out, s in work:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            kb.kimad_mx4_product(a, b, out[2])
+        graphs.append(g)
+    for _ in range(5):
+        for g, w in zip(graphs, work):
+            with torch.cuda.stream(w[4]):
+                g.replay()
+    torch.cuda.synchronize()
+    for _, _, want, out, _ in work:
+        assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+        assert want is None or np.array_equal(out[0].cpu().numpy().astype(np.float64), want)
+
+
+def test_first_calls_of_a_process_can_be_captured():
+    code = """
+import torch
+from paper_2312_08053_b200 import binding as kb
+x = torch.randn((300, 200), device="cuda")
+a, b = kb.Mx4Operand(200, 300), kb.Mx4Operand(300, 200)
+c, d = torch.zeros((200, 200), device="cuda"), torch.zeros((300, 300), device="cuda")
+y = torch.zeros_like(x)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+def calls():
+    kb.kimad_mx4_quantize(x, a, 0)
+    kb.kimad_mx4_quantize(x, b, 1)
+    kb.kimad_mx4_product(a, a, c)
+    kb.kimad_mx4_product(b, b, d)
+    kb.kimad_mx4_dequantize(b, y, 1)
+with torch.cuda.graph(g):
+    calls()
+g.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (c, d, y)]
+calls()
+torch.cuda.synchronize()
+assert all(torch.equal(p, q) and p.any() for p, q in zip(got, (c, d, y)))
+print("captured")
+"""
+    res = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and "captured" in res.stdout, res.stdout[-2000:] + res.stderr[-2000:]
