@@ -1147,7 +1147,8 @@ int mx4_prepare_product() {
     const uint64_t bit = 1ull << (dev & 63);
     if (dev >= 256 || !(raised[dev / 64].load(std::memory_order_acquire) & bit)) {
         CUDA_TRY(cudaFuncSetAttribute(k_mx4_product_parts, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxPartSmem));
-        CUDA_TRY(cudaFuncSetAttribute(k_mx4_product_pairs, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxPairSmem));
+        CUDA_TRY(cudaFuncSetAttribute(k_mx4_product_pairs<5, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, mx_pair_smem(5, 2)));
+        CUDA_TRY(cudaFuncSetAttribute(k_mx4_product_pairs<4, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize, mx_pair_smem(4, 3)));
         if (dev < 256) raised[dev / 64].fetch_or(bit, std::memory_order_release);
     }
     return KIMAD_OK;
@@ -1317,8 +1318,14 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
     { const int rc = mx4_prepare_product(); if (rc != KIMAD_OK) return rc; }
     if (pairs) {
         const uint32_t by_tma = mx4_map_output(&map_out, out_dev, m, n, batch, ld, batch_stride);
-        CUDA_TRY(launch_pdl(k_mx4_product_pairs, dim3((uint32_t)std::min<uint64_t>(pair_tiles, 74) * 2), kMxPairThreads, kMxPairSmem, s, map_a, map_b,
-                            map_out, p, (uint32_t)pair_tiles, by_tma));
+        // with old values to read and a short sum, those are what takes long (2 x 5632 x 2048 outputs over 2048 values: 43.7 us with <5, 2>, 41.8 with <4, 3>; over
+        // 4096 55.8 and 61.5)
+        const bool short_sum = beta != 0.f && rounds <= 10;
+        auto launch = [&](auto kern, size_t smem) {
+            return launch_named("k_mx4_product_pairs", kern, dim3((uint32_t)std::min<uint64_t>(pair_tiles, 74) * 2), kMxPairThreads, smem, s, map_a, map_b, map_out, p,
+                                (uint32_t)pair_tiles, by_tma);
+        };
+        CUDA_TRY(short_sum ? launch(k_mx4_product_pairs<4, 3>, mx_pair_smem(4, 3)) : launch(k_mx4_product_pairs<5, 2>, mx_pair_smem(5, 2)));
     } else {
         CUDA_TRY(launch_clusters("k_mx4_product_parts", parts, k_mx4_product_parts, dim3((uint32_t)all, 1, parts), kMxPartThreads, kMxPartSmem, s, map_a, map_b, p));
     }

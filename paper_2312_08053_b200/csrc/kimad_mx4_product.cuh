@@ -239,12 +239,14 @@ constexpr int kMxPartThreads = 192;    // warps 0-3 scales and outputs, 4 copies
 constexpr uint32_t kMxPartCols = 256;  // of tensor memory: 128 of sums, 16 of scales a stage
 static_assert(kMxPartSmem <= 227 * 1024 && 128 + 16 * kMxPartStages <= kMxPartCols, "memory");
 
-template <uint32_t PARTS> __device__ __forceinline__ void mx_join(uint32_t slab, uint32_t lane, uint32_t (&sums)[32]) {
+// A slab's sums over all parts, in their order: this CTA's own are in `sums`, the others' in shared memory.
+template <uint32_t PARTS> __device__ __forceinline__ void mx_join(uint32_t slab, uint32_t part, uint32_t lane, uint32_t (&sums)[32]) {
 #pragma unroll
     for (uint32_t c = 0; c < 8; ++c) {
         uint4 v[PARTS];
 #pragma unroll
-        for (uint32_t z = 0; z < PARTS; ++z) v[z] = shared4(slab + 4096 * z * (4 / PARTS) + ((c ^ (lane & 7u)) << 4));
+        for (uint32_t z = 0; z < PARTS; ++z)
+            v[z] = z == part ? make_uint4(sums[4 * c], sums[4 * c + 1], sums[4 * c + 2], sums[4 * c + 3]) : shared4(slab + 4096 * z * (4 / PARTS) + ((c ^ (lane & 7u)) << 4));
 #pragma unroll
         for (uint32_t z = 1; z < PARTS; ++z)
             v[0] = make_uint4(mx_add(v[0].x, v[z].x), mx_add(v[0].y, v[z].y), mx_add(v[0].z, v[z].z), mx_add(v[0].w, v[z].w));
@@ -265,14 +267,31 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t warp = warp_number(), lane = threadIdx.x & 31;
     const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u, parts = gridDim.z, part = blockIdx.z;
     const uint32_t full = bar, empty = bar + 8 * S, scaled = bar + 16 * S, done = bar + 24 * S, joined = done + 8; // a stage's copies, products, scales; all products; all parts' sums
-    if (warp == 4 && p.a.blocks && one_lane()) { tma_prefetch(&map_a); tma_prefetch(&map_b); }
-    if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); mbar_init(scaled + 8 * s, 4); }
-        mbar_init(done, 1);
-        mbar_init(joined, 1);
+    const uint32_t bt = blockIdx.x % p.b.line_tiles, at = blockIdx.x / p.b.line_tiles % p.a.line_tiles;
+    const uint32_t n = blockIdx.x / p.b.line_tiles / p.a.line_tiles;
+    const uint32_t all_rounds = (p.a.blocks + kMxStageK / kMxBlock - 1) / (kMxStageK / kMxBlock), tiles = p.a.block_tiles;
+    const uint32_t most = (all_rounds + parts - 1) / parts, first = min(part * most, all_rounds), rounds = min(all_rounds - first, most); // of this CTA
+    uint32_t r = 0; // rounds whose copies, or whose products, have been issued
+    MxRing<S> q;
+    auto bring = [&] { // the next stage's codes
+        const uint32_t to = smem + q.s * kMxPartStageBytes, ready = full + 8 * q.s;
+        if (one_lane()) {
+            mbar_expect(ready, kMxPartStageBytes);
+            tma_load_3d(to, &map_a, (int)((first + r) * 128), (int)(at * kMxTile), (int)n, ready);
+            tma_load_3d(to + kMxOperandStage, &map_b, (int)((first + r) * 128), (int)(bt * kMxTile), (int)n, ready);
+        }
+        ++r;
+        q.next();
+    };
+    if (warp == 4) { // the first copies are under way before the rest of the CTA is ready
+        if (rounds && one_lane()) { tma_prefetch(&map_a); tma_prefetch(&map_b); }
+        if (lane < 3 * S + 2) mbar_init(bar + 8 * lane, lane >= 2 * S && lane < 3 * S ? 4u : 1u); // (in the order of their places)
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        if (parts > 1) mbar_expect(joined, kMxJoin);
+        __syncwarp();
+        if (parts > 1 && one_lane()) mbar_expect(joined, kMxJoin / parts * (parts - 1));
+        pdl_wait();
+        while (r < min(rounds, 2u)) bring();
     }
     if (warp == 5) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kMxPartCols) : "memory");
@@ -285,25 +304,14 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t tmem = s_tmem;
     pdl_wait();
 
-    const uint32_t bt = blockIdx.x % p.b.line_tiles, at = blockIdx.x / p.b.line_tiles % p.a.line_tiles;
-    const uint32_t n = blockIdx.x / p.b.line_tiles / p.a.line_tiles;
-    const uint32_t all_rounds = (p.a.blocks + kMxStageK / kMxBlock - 1) / (kMxStageK / kMxBlock), tiles = p.a.block_tiles;
-    const uint32_t most = (all_rounds + parts - 1) / parts, first = min(part * most, all_rounds), rounds = min(all_rounds - first, most); // of this CTA
-    uint32_t r = 0; // rounds whose copies, or whose products, have been issued
     float was[2][32];
     const MxOutput o(p, n, at * kMxTile + warp * 32, bt * kMxTile, kMxTile, lane); // (of warps 0-3)
     const uint32_t mine = tmem + (warp * 32 << 16);
     bool fine = false;
-    MxRing<S> q;
     if (warp == 4) {
-        for (; r < rounds; ++r, q.next()) {
-            const uint32_t to = smem + q.s * kMxPartStageBytes, ready = full + 8 * q.s;
+        while (r < rounds) {
             if (r >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
-            if (one_lane()) {
-                mbar_expect(ready, kMxPartStageBytes);
-                tma_load_3d(to, &map_a, (int)((first + r) * 128), (int)(at * kMxTile), (int)n, ready);
-                tma_load_3d(to + kMxOperandStage, &map_b, (int)((first + r) * 128), (int)(bt * kMxTile), (int)n, ready);
-            }
+            bring();
         }
     } else if (warp == 5) {
         for (; r < rounds; ++r, q.next()) {
@@ -357,22 +365,26 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     // Sums that the CTAs exchange: slabs of 32 by 32, a warp's four behind each other (CTA 0's for this one, CTA 1's, ..), sixteen bytes c of row i at c ^ (i % 8).
-    // They leave from where the stages were.
+    // They leave from where the stages were; a CTA's own stay in tensor memory.
     const uint32_t in = smem + S * kMxPartStageBytes + warp * 4 * 4096, out = smem + warp * 4 * 4096;
     float* buf = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + kMxJoin) + warp * 32 * 33;
     if (warp < 4 && fine && parts > 1) {
 #pragma unroll 1
         for (uint32_t slab = 0; slab < 4; ++slab) {
+            if (slab % parts == part) continue;
             uint32_t sums[32];
             if (rounds) tc_load32(sums, mine + 32 * slab);
 #pragma unroll
             for (uint32_t c = 0; c < 8; ++c)
                 asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(out + 4096 * slab + lane * 128 + ((c ^ (lane & 7u)) << 4)), "r"(rounds ? sums[4 * c] : 0u),
                              "r"(rounds ? sums[4 * c + 1] : 0u), "r"(rounds ? sums[4 * c + 2] : 0u), "r"(rounds ? sums[4 * c + 3] : 0u) : "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (one_lane())
-                far_copy(shared_of(in + 4096 * (part * (4 / parts) + slab / parts), slab % parts), out + 4096 * slab, 4096, shared_of(joined, slab % parts));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (one_lane()) {
+            for (uint32_t slab = 0; slab < 4; ++slab)
+                if (slab % parts != part)
+                    far_copy(shared_of(in + 4096 * (part * (4 / parts) + slab / parts), slab % parts), out + 4096 * slab, 4096, shared_of(joined, slab % parts));
         }
         fine = mbar_wait(joined, 0, &s_failed);
         __syncwarp();
@@ -383,13 +395,13 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             const uint32_t slab = part + i * parts;
             if (slab >= 4) break;
             uint32_t sums[32];
-            if (parts == 4) mx_join<4>(in + 4096 * i + lane * 128, lane, sums);
-            else if (parts == 2) mx_join<2>(in + 4096 * i + lane * 128, lane, sums);
-            else if (rounds) tc_load32(sums, mine + 32 * slab);
+            if (rounds) tc_load32(sums, mine + 32 * slab);
             else {
 #pragma unroll
                 for (int k = 0; k < 32; ++k) sums[k] = 0;
             }
+            if (parts == 4) mx_join<4>(in + 4096 * i + lane * 128, part, lane, sums);
+            else if (parts == 2) mx_join<2>(in + 4096 * i + lane * 128, part, lane, sums);
             o.put(slab, sums, was[i & 1], buf);
             if (i < 2 && slab + 2 * parts < 4) o.fetch(slab + 2 * parts, was[i & 1]);
         }
@@ -422,16 +434,13 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // Warps: 0-7 outputs (a quarter of the lines and half of the columns each), 8-11 scales to tensor memory, 12 copies of codes, 14 of scales (a copy takes
 // almost 100 clocks to issue; all five of a stage in one warp are more than its products take), 13 products (in the pair's first CTA).
 constexpr uint32_t kMxPairN = 192;
-constexpr uint32_t kMxPairStages = 5;
 constexpr uint32_t kMxPairBytesB = kMxPairN / 2 * 128;
 constexpr uint32_t kMxPairScales = 2 * 512; // bytes of a stage's scales of a tile of lines; of A's one and of B's two
 constexpr uint32_t kMxPairStageBytes = kMxOperandStage + kMxPairBytesB + 3 * kMxPairScales;
-constexpr uint32_t kMxPairOut = 2 * 4096; // bytes of a warp's outputs: two slabs of 32 by 32, or one of 32 by 33
-constexpr uint32_t kMxPairSmem = 1024 + kMxPairStages * kMxPairStageBytes + 8 * kMxPairOut;
+KIMAD_HD constexpr uint32_t mx_pair_smem(uint32_t stages, uint32_t slabs) { return 1024 + stages * kMxPairStageBytes + 8 * slabs * 4096; }
 constexpr int kMxPairThreads = 480;
 constexpr uint32_t kMxPairScaleCols = 24; // of a stage: A's 2 x 4, B's 2 x 8 (6 in use)
-static_assert(2 * kMxPairN + kMxPairStages * kMxPairScaleCols <= 512, "tensor memory");
-static_assert(kMxPairSmem <= 227 * 1024 && kMxPairStageBytes % 1024 == 0 && kMxPairN == 192, "shared memory; tc_store_scales");
+static_assert(kMxPairStageBytes % 1024 == 0 && kMxPairN == 192, "shared memory; tc_store_scales");
 
 // Arrival on the barrier of the pair's first CTA.  Relaxed: what is handed over are accesses to tensor memory that have been waited for (tcgen05.wait) and
 // copies that have been, none of the thread's own writes; with release the arrival waits for every store under way, about 1000 clocks.
@@ -458,12 +467,16 @@ struct MxPairTile {
     }
 };
 
+// S stages and, for each output warp, SLABS slabs under way.  More stages hide more of the copies' way from L2 (5632 x 5632 outputs over 8192 values with three,
+// four, five stages: 131, 115, 108 us), more slabs more of the old values' (2 x 5632 x 2048 outputs and as many old values over 64 with two, three: 38.0, 34.4;
+// over 1024: 41.2, 38.2).
+template <uint32_t S, uint32_t SLABS>
 __global__ void __launch_bounds__(kMxPairThreads, 1) __cluster_dims__(2, 1, 1)
 k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
                     const __grid_constant__ MxProduct p, uint32_t all_tiles, uint32_t by_tma) {
     extern __shared__ uint8_t smem_raw[];
-    constexpr uint32_t S = kMxPairStages;
-    __shared__ __align__(8) uint64_t s_bar[3 * S + 5 + 16];
+    static_assert(2 * kMxPairN + S * kMxPairScaleCols <= 512 && mx_pair_smem(S, SLABS) <= 227 * 1024 && SLABS <= kMxPairN / 64, "tensor memory, shared memory");
+    __shared__ __align__(8) uint64_t s_bar[3 * S + 5 + 8 * SLABS];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
     const uint32_t warp = warp_number(), lane = threadIdx.x & 31, rank = cluster_rank();
@@ -471,7 +484,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     // a stage's copies are here; its scales are in tensor memory, in both CTAs (first CTA); its products are done; a tile's products are done; its sums
     // have been read, in both CTAs (first CTA); everything issued is done
     const uint32_t full = bar, ready = bar + 8 * S, empty = bar + 16 * S, done = bar + 24 * S, drained = done + 16, quit = done + 32,
-                   old = quit + 8; // (an output warp's slabs of old values: two each)
+                   old = quit + 8; // (an output warp's slabs of old values, SLABS each)
     if (warp == 12 && one_lane()) {
         tma_prefetch(&map_a);
         tma_prefetch(&map_b);
@@ -481,7 +494,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 2); mbar_init(ready + 8 * s, 8); mbar_init(empty + 8 * s, 1); }
         for (uint32_t b = 0; b < 2; ++b) { mbar_init(done + 8 * b, 1); mbar_init(drained + 8 * b, 16); }
         mbar_init(quit, 1);
-        for (uint32_t i = 0; i < 16; ++i) mbar_init(old + 8 * i, 1);
+        for (uint32_t i = 0; i < 8 * SLABS; ++i) mbar_init(old + 8 * i, 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -585,10 +598,10 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (warp < 8) {
         const uint32_t quarter = warp & 3u, half = warp >> 2;
         constexpr uint32_t kSlabs = kMxPairN / 64;
-        const uint32_t slabs = smem + S * kMxPairStageBytes + warp * kMxPairOut;
+        const uint32_t slabs = smem + S * kMxPairStageBytes + warp * SLABS * 4096;
         float* buf = reinterpret_cast<float*>(smem_raw + (slabs - smem_u32(smem_raw)));
-        MxRing<2> u;     // places of sums
-        MxRing<2> w, l;  // slabs worked on, slabs whose old values are asked for
+        MxRing<2> u;        // places of sums
+        MxRing<SLABS> w, l; // slabs worked on, slabs whose old values are asked for
         for (uint32_t tile = pair; tile < all_tiles; tile += pairs, u.next()) {
             const MxPairTile t(p, tile);
             const uint32_t sums_at = tmem + (quarter * 32 << 16) + u.s * kMxPairN + half * (kMxPairN / 2);
@@ -598,14 +611,15 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             auto ask = [&](uint32_t slab) { // for a slab's old values, in a place whose last store has been read
                 if (lane == 0) {
                     tma_stores_read<0>();
-                    mbar_expect(old + 8 * (2 * warp + l.s), 4096);
-                    tma_load_3d(slabs + 4096 * l.s, &map_out, col + 32 * (int)slab, row, (int)t.n, old + 8 * (2 * warp + l.s));
+                    mbar_expect(old + 8 * (SLABS * warp + l.s), 4096);
+                    tma_load_3d(slabs + 4096 * l.s, &map_out, col + 32 * (int)slab, row, (int)t.n, old + 8 * (SLABS * warp + l.s));
                 }
                 l.next();
             };
             if (p.beta != 0.f) {
-                if (mine > 0) ask(0);
-                if (mine > 1) ask(1);
+#pragma unroll
+                for (uint32_t i = 0; i < SLABS; ++i)
+                    if (i < mine) ask(i);
             }
             if (!mbar_wait(done + 8 * u.s, u.parity, &s_failed) || s_failed) break;
             __syncwarp();
@@ -628,9 +642,9 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 // sixteen bytes c of row r lie at c ^ (r % 8): no two of eight lanes meet in a bank
                 const uint32_t at = slabs + 4096 * w.s + lane * 128;
                 if (p.beta != 0.f) {
-                    if (!mbar_wait(old + 8 * (2 * warp + w.s), w.parity, &s_failed)) break;
+                    if (!mbar_wait(old + 8 * (SLABS * warp + w.s), w.parity, &s_failed)) break;
                 } else {
-                    if (lane == 0) tma_stores_read<1>(); // the other place's store may still be under way
+                    if (lane == 0) tma_stores_read<SLABS - 1>(); // the other places' stores may still be under way
                 }
                 __syncwarp();
 #pragma unroll
@@ -648,13 +662,13 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 __syncwarp();
                 if (lane == 0) tma_store_3d(&map_out, col + 32 * (int)slab, row, (int)t.n, slabs + 4096 * w.s);
                 w.next();
-                if (p.beta != 0.f && slab + 2 < mine) ask(slab + 2);
+                if (p.beta != 0.f && slab + SLABS < mine) ask(slab + SLABS);
             }
         }
         if (p.beta != 0.f) { // (after a failure: values asked for and not waited for)
             const long long began = clock64();
             for (; w.s != l.s || w.parity != l.parity; w.next())
-                while (!mbar_try(old + 8 * (2 * warp + w.s), w.parity) && clock64() - began < kMxWaitClocks) {}
+                while (!mbar_try(old + 8 * (SLABS * warp + w.s), w.parity) && clock64() - began < kMxWaitClocks) {}
         }
         if (by_tma && lane == 0) tma_stores_done();
         __syncwarp();

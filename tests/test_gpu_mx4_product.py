@@ -55,7 +55,7 @@ SHAPES = [(1, 1, 1, 1), (1, 128, 128, 64), (1, 128, 128, 256), (1, 7, 300, 33), 
           (1, 256, 200, 3073), (1, 130, 129, 4097), (2, 70, 60, 4351), (9, 200, 256, 4100), (1, 1, 1, 3329), (36, 128, 128, 4096),
           # outputs on 16 bytes and smaller than a slab; cut tiles of 256 x 192, whole ones, more tiles than pairs of SMs, more rounds than stages
           (3, 5, 8, 100), (1, 40, 36, 70), (2, 300, 12, 65), (2, 300, 200, 2000), (1, 520, 400, 1500),
-          (1, 2560, 1536, 64), (40, 130, 200, 300), (80, 20, 30, 511), (1, 2500, 2000, 33), (3, 1300, 1000, 1000), (19, 257, 193, 900), (76, 256, 192, 256)]
+          (1, 2560, 1536, 64), (40, 130, 200, 300), (80, 20, 30, 511), (1, 2500, 2000, 33), (3, 1300, 1000, 1000), (19, 257, 193, 900), (3, 1300, 1000, 2900), (76, 256, 192, 256)]
 
 
 @pytest.mark.parametrize("batch,m,n,length", SHAPES)
