@@ -17,7 +17,8 @@
  *
  * Beside it: the receiving side of a message and the model step (kimad_apply_packed, kimad_aggregate:
  * Algorithm 1, server lines), and, through kimad_options.policy, Kimad without layer adaptivity
- * (Section 3.1) and the error-axis reading of Algorithm 3.
+ * (Section 3.1) and the error-axis reading of Algorithm 3.  Quantisation, the paper's other family of compressors, has the same pass
+ * with microscaled 4-bit floats, its receiving side, and products of matrices so quantised (kimad_mx4_*).
  *
  * Conventions
  *   - L layers of sizes n_l, concatenated in list order into one flat vector of N elements.

@@ -21,8 +21,9 @@
 //                   (d) exact threshold and per-slice output offsets at the chosen k             [kimad_select.cuh]
 //   k_sel_write     (e)+(f) ordered (index, value) pack and g += C(d) (Algorithm 1, Eq. 6)       [kimad_select.cuh]
 //   k_apply_packed, k_aggregate   receiving side and model step (Algorithm 1, server lines)      [kimad_receiver.cuh]
+//   k_mx4_*         the same pass with a 4-bit quantiser, and products of quantised matrices        [kimad_mx4.cuh, kimad_mx4_product.cuh]
 //
-// Nothing here is a dense contraction, so there is no tensor-core path.  The sweep runs at 83-90 % of the measured HBM
+// Nothing here but the products is a dense contraction, so there is no other tensor-core path.  The sweep runs at 83-90 % of the measured HBM
 // copy rate on its 9 bytes per element (one shared-memory table read and two shared-memory atomics per element keep it
 // from the rest); the counting and write sweeps are bound by HBM on large layers and by load latency on small ones.
 // After the sample kernel the workers go through the stages as two groups on streams of their own (kimad_api.cu).
