@@ -301,11 +301,17 @@ int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, vo
  * taken in binary32 on the tensor cores (products of codes exactly, at most one rounding per 32 values and addition), always in the same
  * order; then fl32(alpha sum), with beta != 0 fl32(beta out + that) with one rounding; with beta = 0 out is not read.  Blocks of scale 255 make NaN of their
  * line's outputs.  length 0: out <- beta out.  What lies between rows and matrices is left as it is.
- * status_dev: device i32 or NULL; set to KIMAD_ERR_TIMEOUT if a bounded wait inside the kernel ran out (its tile is then not written), else left as it is.
+ * status_dev: device i32 or NULL; set to KIMAD_ERR_TIMEOUT if a bounded wait inside the kernel ran out (some outputs are then left as they were), else left
+ * as it is.
  * Asynchronous on cuda_stream; no context, no workspace.  m, n or batch 0: nothing is done.  Errors: INVALID_ARG, CUDA. */
 int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64_t m, uint64_t n, uint64_t length, uint64_t batch, const uint8_t* a_codes_dev,
                       const uint8_t* a_scales_dev, const uint8_t* b_codes_dev, const uint8_t* b_scales_dev, float alpha, float beta, int32_t* status_dev,
                       void* cuda_stream);
+
+/* Limit, in SM clocks, of the waits inside the product's kernels, for all calls of the process from now on (default and maximum 2^31, about a second).  For
+ * tests: with withhold != 0 the kernels do not bring their operands, so that what they wait for never comes and the limit is what ends them;
+ * the call sets its status and leaves its outputs as they were.  Errors: INVALID_ARG. */
+int kimad_debug_mx4_set_wait_limit(uint64_t clocks, int withhold);
 
 /* ---- Bandwidth monitor (Section 2.4: every device estimates its bandwidth B_m^k from what it observed; the
  * paper gives no formula, this is ours).  Host-only, no GPU.  The caller reports every finished transfer (the

@@ -145,6 +145,8 @@ def load():
     L.kimad_mx4_quantize.argtypes = [vp, u32, u64, u64, u64, u64, u64, u32, vp, vp, vp]
     L.kimad_mx4_dequantize.restype = C.c_int
     L.kimad_mx4_dequantize.argtypes = [vp, vp, vp, u32, u64, u64, u64, u64, u64, u32, vp]
+    L.kimad_debug_mx4_set_wait_limit.restype = C.c_int
+    L.kimad_debug_mx4_set_wait_limit.argtypes = [u64, C.c_int]
     L.kimad_mx4_product.restype = C.c_int
     L.kimad_mx4_product.argtypes = [vp] + [u64] * 6 + [vp] * 4 + [C.c_float, C.c_float, vp, vp]
     L.kimad_monitor_create.restype = C.c_int
@@ -628,6 +630,11 @@ def kimad_mx4_product(a: Mx4Operand, b: Mx4Operand, out, alpha=1.0, beta=0.0, st
         _mx4_stream("kimad_mx4_product", stream, status.get_device())
     _check((_lib or load()).kimad_mx4_product(out.data_ptr(), ld, bs, a.lines, b.lines, a.length, a.batch, a.codes_ptr, a.scales_ptr,
                                     b.codes_ptr, b.scales_ptr, alpha, beta, None if status is None else status.data_ptr(), s), "kimad_mx4_product")
+
+
+def kimad_debug_mx4_set_wait_limit(clocks: int, withhold: bool = False) -> None:
+    """Limit of the waits inside the product's kernels in SM clocks, 2^31 by default; withhold: let them run out (see kimad.h)."""
+    _check(load().kimad_debug_mx4_set_wait_limit(int(clocks), int(bool(withhold))), "kimad_debug_mx4_set_wait_limit")
 
 
 class Monitor:

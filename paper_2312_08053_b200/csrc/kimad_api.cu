@@ -1125,6 +1125,9 @@ bool mx4_operand_ok(uint64_t lines, uint64_t length, uint64_t batch, const void*
     return tiles <= 0x7fffffffull && (tiles == 0 || batch <= 0x7fffffffull / tiles);
 }
 
+std::atomic<long long> g_mx4_wait_clocks{kMxWaitClocks}; // kimad_debug_mx4_set_wait_limit
+std::atomic<uint32_t> g_mx4_withhold{0};
+
 // cuTensorMapEncodeTiled, by way of the runtime: the library is not linked against the driver.
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -1303,7 +1306,7 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
         return KIMAD_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const MxProduct p{out_dev, ld, batch_stride, a_scales_dev, b_scales_dev, MxOperand((uint32_t)m, (uint32_t)length), MxOperand((uint32_t)n, (uint32_t)length),
-                      alpha, beta, status_dev};
+                      alpha, beta, status_dev, g_mx4_wait_clocks.load(std::memory_order_relaxed), g_mx4_withhold.load(std::memory_order_relaxed)};
     const uint64_t tiles = (uint64_t)p.a.line_tiles * p.b.line_tiles;
     if (tiles > 0x7fffffffull || batch > 0x7fffffffull / tiles) return KIMAD_ERR_INVALID_ARG;
     const uint64_t pair_tiles = (m + 255) / 256 * ((n + kMxPairN - 1) / kMxPairN) * batch, all = tiles * batch, rounds = (p.a.blocks + 7) / 8;
@@ -1330,6 +1333,13 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
         CUDA_TRY(launch_clusters("k_mx4_product_parts", parts, k_mx4_product_parts, dim3((uint32_t)all, 1, parts), kMxPartThreads, kMxPartSmem, s, map_a, map_b, p));
     }
     CUDA_TRY(cudaGetLastError());
+    return KIMAD_OK;
+}
+
+int kimad_debug_mx4_set_wait_limit(uint64_t clocks, int withhold) {
+    if (clocks > (uint64_t)kMxWaitClocks) return KIMAD_ERR_INVALID_ARG;
+    g_mx4_wait_clocks.store((long long)clocks, std::memory_order_relaxed);
+    g_mx4_withhold.store(withhold != 0, std::memory_order_relaxed);
     return KIMAD_OK;
 }
 

@@ -21,7 +21,7 @@ namespace kimad {
 
 constexpr uint32_t kMxStageK = 256;                  // values of the summed axis in a stage
 constexpr uint32_t kMxOperandStage = 128 * 128;      // bytes of codes of an operand in a stage
-constexpr long long kMxWaitClocks = 1ll << 31;       // about a second
+constexpr long long kMxWaitClocks = 1ll << 31;       // about a second: the limit of a wait, by default, and of those after a failure
 
 // Instruction descriptor of kind mxf4: E2M1 by E2M1, scales UE8M0, K-major, N (bits 17-22, in eights), M (bits 27-28, in 128s).
 // The two scales of a product lie in bytes 0-1 or 2-3 of their column (bits 4-5 for B, 29-30 for A).
@@ -42,13 +42,19 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-// Bounded: false when the phase has not ended within the limit or another warp of the CTA has given up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
-    if (mbar_try(bar, parity)) return true;
+// Waits of whole warps, bounded: false, for all lanes, when the phase has not ended within the limit or another warp of the CTA has given up.
+struct MxWait {
+    volatile uint32_t* flag;
+    long long clocks;
+    __device__ __forceinline__ bool failed() const { return __any_sync(0xffffffffu, *flag != 0); }
+};
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const MxWait& w) {
+    bool ended = mbar_try(bar, parity);
+    if (__all_sync(0xffffffffu, ended)) return true;
     const long long began = clock64();
-    while (!mbar_try(bar, parity))
-        if (*failed || clock64() - began > kMxWaitClocks) { *failed = 1; return false; }
-    return true;
+    while (!ended && !(ended = mbar_try(bar, parity)))
+        if (*w.flag || clock64() - began > w.clocks) { *w.flag = 1; break; }
+    return __all_sync(0xffffffffu, ended);
 }
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -122,6 +128,8 @@ struct MxProduct {
     MxOperand a, b;
     float alpha, beta;
     int32_t* status;
+    long long wait_clocks;
+    uint32_t withhold; // codes are not copied, so that waits run out
 };
 
 // A warp's part of the output, 32 rows by slabs of 32 columns.  A lane has a row of the sums, as tensor memory gives them.  Where the output's rows lie on
@@ -264,6 +272,7 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     __shared__ __align__(8) uint64_t s_bar[3 * S + 2];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
+    const MxWait wait{&s_failed, p.wait_clocks};
     const uint32_t warp = warp_number(), lane = threadIdx.x & 31;
     const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u, parts = gridDim.z, part = blockIdx.z;
     const uint32_t full = bar, empty = bar + 8 * S, scaled = bar + 16 * S, done = bar + 24 * S, joined = done + 8; // a stage's copies, products, scales; all products; all parts' sums
@@ -291,7 +300,7 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         __syncwarp();
         if (parts > 1 && one_lane()) mbar_expect(joined, kMxJoin / parts * (parts - 1));
         pdl_wait();
-        while (r < min(rounds, 2u)) bring();
+        while (r < min(rounds, 2u) && !p.withhold) bring();
     }
     if (warp == 5) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kMxPartCols) : "memory");
@@ -309,15 +318,15 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t mine = tmem + (warp * 32 << 16);
     bool fine = false;
     if (warp == 4) {
-        while (r < rounds) {
-            if (r >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
+        while (r < rounds && !p.withhold) {
+            if (r >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, wait)) break;
             bring();
         }
     } else if (warp == 5) {
         for (; r < rounds; ++r, q.next()) {
             const uint32_t scales = tmem + kMxTile + 16 * q.s;
             const uint64_t a = mx_desc_codes(smem + q.s * kMxPartStageBytes), b = mx_desc_codes(smem + q.s * kMxPartStageBytes + kMxOperandStage);
-            if (!mbar_wait(scaled + 8 * q.s, q.parity, &s_failed)) break; // ... which the warps that stored them have waited for `full` with
+            if (!mbar_wait(scaled + 8 * q.s, q.parity, wait)) break; // ... which the warps that stored them have waited for `full` with
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t products = min((p.a.blocks - (first + r) * 8 + 1) / 2, 4u); // of 64 values, two blocks, each
             if (one_lane()) {
@@ -339,7 +348,7 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             }
         };
         auto store = [&](const uint4 (&v)[4]) {
-            if (!mbar_wait(full + 8 * q.s, q.parity, &s_failed)) return false; // (and so the products that used the scales' place before are done)
+            if (!mbar_wait(full + 8 * q.s, q.parity, wait)) return false; // (and so the products that used the scales' place before are done)
             __syncwarp();
             tc_store16(mine + kMxTile + 16 * q.s, v);
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -359,7 +368,7 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             if (i + 1 >= rounds || !store(v1)) break;
             load(i + 3, v1);
         }
-        fine = mbar_wait(done, 0, &s_failed) && !s_failed;
+        fine = mbar_wait(done, 0, wait) && !wait.failed();
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     }
     __syncwarp();
@@ -386,7 +395,7 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if (slab % parts != part)
                     far_copy(shared_of(in + 4096 * (part * (4 / parts) + slab / parts), slab % parts), out + 4096 * slab, 4096, shared_of(joined, slab % parts));
         }
-        fine = mbar_wait(joined, 0, &s_failed);
+        fine = mbar_wait(joined, 0, wait);
         __syncwarp();
     }
     if (warp < 4 && fine) {
@@ -416,6 +425,8 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 while (!mbar_try(full + 8 * (i % S), (i / S) & 1u) && clock64() - began < kMxWaitClocks) {}
         if (warp == 5 && lane == 0)
             while (!mbar_try(done, 0) && clock64() - began < kMxWaitClocks) {}
+        if (warp == 0 && lane == 0 && parts > 1)
+            while (!mbar_try(joined, 0) && clock64() - began < kMxWaitClocks) {}
         __syncwarp();
     }
     cluster_sync(); // the copies from this CTA's memory have arrived
@@ -479,6 +490,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     __shared__ __align__(8) uint64_t s_bar[3 * S + 5 + 8 * SLABS];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
+    const MxWait wait{&s_failed, p.wait_clocks};
     const uint32_t warp = warp_number(), lane = threadIdx.x & 31, rank = cluster_rank();
     const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // a stage's copies are here; its scales are in tensor memory, in both CTAs (first CTA); its products are done; a tile's products are done; its sums
@@ -514,11 +526,11 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     uint32_t it = 0; // stages whose copies, or whose products, have been issued
     MxRing<S> q;
     if (warp == 12) {
-        for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
+        for (uint32_t tile = pair; tile < all_tiles && !p.withhold && !wait.failed(); tile += pairs) {
             const MxPairTile t(p, tile);
             for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
                 const uint32_t to = smem + q.s * kMxPairStageBytes, here = full + 8 * q.s;
-                if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
+                if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, wait)) break;
                 if (one_lane()) {
                     mbar_expect(here, kMxOperandStage + kMxPairBytesB);
                     tma_load_3d(to, &map_a, (int)(r * 128), (int)(t.row + rank * kMxTile), (int)t.n, here);
@@ -527,7 +539,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             }
         }
     } else if (warp == 14) {
-        for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
+        for (uint32_t tile = pair; tile < all_tiles && !wait.failed(); tile += pairs) {
             const MxPairTile t(p, tile);
             const uint32_t la = t.row / kMxTile + rank, lb = t.col / kMxTile; // tiles of lines whose scales are read
             const bool have_a = la < p.a.line_tiles, have_b = lb + 1 < p.b.line_tiles;
@@ -535,7 +547,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             const uint8_t* sb = p.scales_b + ((uint64_t)t.n * p.b.line_tiles + lb) * tiles * 512;
             for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
                 const uint32_t to = smem + q.s * kMxPairStageBytes + kMxOperandStage + kMxPairBytesB, here = full + 8 * q.s;
-                if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, &s_failed)) break;
+                if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, wait)) break;
                 if (one_lane()) {
                     const uint32_t bytes = min(tiles - 2 * r, 2u) * 512u;
                     mbar_expect(here, bytes * (1u + have_a + have_b));
@@ -548,14 +560,14 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     } else if (warp == 13 && rank == 0) {
         MxRing<2> u; // places of sums
         uint32_t j = 0; // tiles of this pair
-        for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs, ++j, u.next()) {
+        for (uint32_t tile = pair; tile < all_tiles && !wait.failed(); tile += pairs, ++j, u.next()) {
             const uint32_t sums = tmem + u.s * kMxPairN;
-            if (j >= 2 && !mbar_wait(drained + 8 * u.s, u.parity ^ 1u, &s_failed)) break;
+            if (j >= 2 && !mbar_wait(drained + 8 * u.s, u.parity ^ 1u, wait)) break;
             for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
                 const uint32_t scales = tmem + 2 * kMxPairN + kMxPairScaleCols * q.s;
                 const uint64_t a = mx_desc_codes(smem + q.s * kMxPairStageBytes), b = mx_desc_codes(smem + q.s * kMxPairStageBytes + kMxOperandStage);
                 const uint32_t products = min((p.a.blocks - r * 8 + 1) / 2, 4u); // of 64 values, two blocks, each
-                if (!mbar_wait(ready + 8 * q.s, q.parity, &s_failed)) break;
+                if (!mbar_wait(ready + 8 * q.s, q.parity, wait)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (one_lane()) {
 #pragma unroll
@@ -565,18 +577,19 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     tc_commit<2>(empty + 8 * q.s);
                 }
             }
+            if (wait.failed()) break; // (an unfinished tile is not announced: the other CTA may not know of the failure)
             if (one_lane()) tc_commit<2>(done + 8 * u.s);
         }
-        if (s_failed && one_lane()) tc_commit<2>(quit);
+        if (wait.failed() && one_lane()) tc_commit<2>(quit);
     } else if (warp >= 8 && warp < 12) {
         const uint32_t mine = tmem + ((warp - 8) * 32 << 16) + 2 * kMxPairN;
-        for (uint32_t tile = pair; tile < all_tiles && !s_failed; tile += pairs) {
+        for (uint32_t tile = pair; tile < all_tiles && !wait.failed(); tile += pairs) {
             const MxPairTile t(p, tile);
             // this lane's words of B's lines, 64 by 64: the first ones may be a tile's second half
             const uint32_t b0 = kMxPairScales + t.col % kMxTile / 64 * 8, b1 = b0 & 8u ? 2 * kMxPairScales : b0 + 8, b2 = b0 & 8u ? b1 + 8 : 2 * kMxPairScales;
             for (uint32_t r = 0; r < rounds; ++r, q.next()) {
                 const uint32_t from = smem + q.s * kMxPairStageBytes + kMxOperandStage + kMxPairBytesB + lane * 16;
-                if (!mbar_wait(full + 8 * q.s, q.parity, &s_failed)) break; // (and so the products that used the scales' place before are done)
+                if (!mbar_wait(full + 8 * q.s, q.parity, wait)) break; // (and so the products that used the scales' place before are done)
                 uint4 a[2];
                 uint2 b[6];
 #pragma unroll
@@ -602,7 +615,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         float* buf = reinterpret_cast<float*>(smem_raw + (slabs - smem_u32(smem_raw)));
         MxRing<2> u;        // places of sums
         MxRing<SLABS> w, l; // slabs worked on, slabs whose old values are asked for
-        for (uint32_t tile = pair; tile < all_tiles; tile += pairs, u.next()) {
+        for (uint32_t tile = pair; tile < all_tiles && !wait.failed(); tile += pairs, u.next()) {
             const MxPairTile t(p, tile);
             const uint32_t sums_at = tmem + (quarter * 32 << 16) + u.s * kMxPairN + half * (kMxPairN / 2);
             const MxOutput o(p, t.n, t.row + rank * kMxTile + quarter * 32, t.col + half * (kMxPairN / 2), kMxPairN / 2, lane);
@@ -621,7 +634,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 for (uint32_t i = 0; i < SLABS; ++i)
                     if (i < mine) ask(i);
             }
-            if (!mbar_wait(done + 8 * u.s, u.parity, &s_failed) || s_failed) break;
+            if (!mbar_wait(done + 8 * u.s, u.parity, wait) || wait.failed()) break;
             __syncwarp();
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -642,7 +655,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 // sixteen bytes c of row r lie at c ^ (r % 8): no two of eight lanes meet in a bank
                 const uint32_t at = slabs + 4096 * w.s + lane * 128;
                 if (p.beta != 0.f) {
-                    if (!mbar_wait(old + 8 * (SLABS * warp + w.s), w.parity, &s_failed)) break;
+                    if (!mbar_wait(old + 8 * (SLABS * warp + w.s), w.parity, wait)) break;
                 } else {
                     if (lane == 0) tma_stores_read<SLABS - 1>(); // the other places' stores may still be under way
                 }
@@ -678,7 +691,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (s_failed) { // what was issued still writes to the pair's shared and tensor memory
         if (threadIdx.x == 0 && p.status) *p.status = KIMAD_ERR_TIMEOUT;
         const long long began = clock64();
-        if (warp == 12 && lane == 0)
+        if ((warp == 12 || warp == 14) && lane == 0) // (a stage of which only one of them has issued its copies does not end, but they do within the limit)
             for (uint32_t i = it > S ? it - S : 0; i < it; ++i)
                 while (!mbar_try(full + 8 * (i % S), (i / S) & 1u) && clock64() - began < kMxWaitClocks) {}
         if (warp == 13 && lane == 0 && rank == 0)

@@ -284,3 +284,25 @@ print("captured")
 """
     res = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert res.returncode == 0 and "captured" in res.stdout, res.stdout[-2000:] + res.stderr[-2000:]
+
+
+@pytest.mark.parametrize("m,n,length", [(600, 500, 700), (128, 128, 8192)])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(m, n, length):
+    """By pairs and by parts: the operands are not brought, so every wait for them ends at its limit (0.1 ms).  Nothing is written, and the GPU goes on."""
+    rng = np.random.default_rng(11)
+    a, va = operand(exact_matrix((1, m, length), rng))
+    b, vb = operand(exact_matrix((1, n, length), rng))
+    want = torch.from_numpy((va[0] @ vb[0].T).astype(np.float32)).cuda()
+    for beta in (0.0, 1.0):
+        out, status = torch.full((m, n), 3.0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        kb.kimad_debug_mx4_set_wait_limit(200000, withhold=True)
+        try:
+            kb.kimad_mx4_product(a, b, out, beta=beta, status=status)
+            torch.cuda.synchronize()
+        finally:
+            kb.kimad_debug_mx4_set_wait_limit(1 << 31)
+        assert int(status) == kb.KIMAD_ERR_TIMEOUT and (out == 3.0).all()
+    status.zero_()
+    kb.kimad_mx4_product(a, b, out, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and (torch.equal(out, want) if length <= 3000 else torch.allclose(out, want, rtol=1e-5, atol=1e-2 * length))

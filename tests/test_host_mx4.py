@@ -186,3 +186,11 @@ def test_binding_refuses_products_of_what_does_not_fit():
             kb.kimad_mx4_product(a, b, out)
     with pytest.raises(TypeError):
         kb.kimad_mx4_product(op(5, 40), op(7, 40), torch.zeros(5, 7, dtype=torch.bfloat16))
+
+
+def test_wait_limit_is_validated():
+    kb.kimad_debug_mx4_set_wait_limit(5, withhold=True)
+    kb.kimad_debug_mx4_set_wait_limit(1 << 31)
+    with pytest.raises(kb.KimadError) as e:
+        kb.kimad_debug_mx4_set_wait_limit((1 << 31) + 1)
+    assert e.value.code == BAD
