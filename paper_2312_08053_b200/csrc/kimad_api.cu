@@ -129,7 +129,7 @@ void plan_layout(kimad_ctx* c) {
     // work lists, one set per group of workers
     y.fb = take(kGroups * align_up(sizeof(FbList)));
     y.rc = take(kGroups * align_up(sizeof(Recount)));
-    y.flags = take((size_t)c->W * sizeof(uint32_t));
+    y.flags = take((size_t)c->W * 2 * sizeof(uint32_t)); // and the CTAs of a 4-bit pass that have arrived
     y.cell_tab = take(WR * kCellTab * sizeof(uint32_t));
     y.cell_win = take(WR * sizeof(int4));
     y.bin_lo = take(WR * (kMaxBins + 1) * sizeof(uint32_t));
@@ -1125,6 +1125,11 @@ bool mx4_operand_ok(uint64_t lines, uint64_t length, uint64_t batch, const void*
     return tiles <= 0x7fffffffull && (tiles == 0 || batch <= 0x7fffffffull / tiles);
 }
 
+// Whether the matrices of a batch of outputs lie apart (whatever their strides).
+bool mx4_apart(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t batch, uint64_t batch_stride) {
+    return batch <= 1 || (unsigned __int128)(rows - 1) * ld + cols <= batch_stride;
+}
+
 std::atomic<long long> g_mx4_wait_clocks{kMxWaitClocks}; // kimad_debug_mx4_set_wait_limit
 std::atomic<uint32_t> g_mx4_withhold{0};
 
@@ -1196,16 +1201,16 @@ int kimad_mx4_step(kimad_ctx* c, const void* grads_dev, uint32_t grad_dtype, flo
     const uint32_t nch = (uint32_t)c->chunks.size(), lp = mx4_log_pieces((uint64_t)nch * c->W);
     const Chunk* chunks = c->at<Chunk>(c->lay.chunks);
     const LayerDesc* layers = c->at<LayerDesc>(c->lay.layers);
-    MxPartial* partial = c->at<MxPartial>(c->lay.csel); // (the selection of a TopK step is over when this runs, and starts from its own counts)
+    // the sums lie where the selection of a TopK step keeps its counts: that is over when this runs, and starts from its own
+    const MxStats st{c->at<MxPartial>(c->lay.csel), lp ? c->at<uint32_t>(c->lay.flags) + c->W : nullptr, out->err, out->stats, c->N, c->blocks * 17, c->L, c->check_finite};
     auto launch = [&](auto kern, auto* grads) {
-        return launch_named("k_mx4_step", kern, dim3(nch << lp, c->W), kThreads, 0, s, grads, state_dev, c->stride, chunks, layers, lp, mx4_buffers(c, out), partial);
+        return launch_named("k_mx4_step", kern, dim3(nch << lp, c->W), kThreads, 0, s, grads, state_dev, c->stride, chunks, layers, lp, mx4_buffers(c, out), st);
     };
     CUDA_TRY(grad_dtype == KIMAD_F32 ? launch(k_mx4_step<float>, static_cast<const float*>(grads_dev))
              : grad_dtype == KIMAD_BF16 ? launch(k_mx4_step<__nv_bfloat16>, static_cast<const __nv_bfloat16*>(grads_dev))
                                         : launch(k_mx4_step<__half>, static_cast<const __half*>(grads_dev)));
-    CUDA_TRY(launch_pdl(k_mx4_stats, c->W, kMxStatsThreads, 0, s, partial, layers, c->L, nch, lp, c->N, c->blocks * 17, c->check_finite, out->err,
-                        out->stats));
-    c->launches += 2;
+    if (!lp) CUDA_TRY(launch_pdl(k_mx4_stats, c->W, kMxStatsThreads, 0, s, st, layers, nch, lp));
+    c->launches += lp ? 1 : 2;
     CUDA_TRY(cudaGetLastError());
     return KIMAD_OK;
 }
@@ -1279,7 +1284,7 @@ int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, vo
         (uintptr_t)x_dev % (dtype == KIMAD_F32 ? 4 : 2))
         return KIMAD_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0 || batch == 0) return KIMAD_OK;
-    if (!x_dev || !codes_dev || !scales_dev || (batch > 1 && batch_stride < (rows - 1) * ld + cols)) return KIMAD_ERR_INVALID_ARG; // outputs on top of each other
+    if (!x_dev || !codes_dev || !scales_dev || !mx4_apart(rows, cols, ld, batch, batch_stride)) return KIMAD_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const MxOperand op((uint32_t)lines, (uint32_t)length);
     auto launch = [&](auto* x) {
@@ -1302,7 +1307,7 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
         !mx4_operand_ok(n, length, batch, b_codes_dev, b_scales_dev))
         return KIMAD_ERR_INVALID_ARG;
     if (m == 0 || n == 0 || batch == 0) return KIMAD_OK;
-    if (!out_dev || (length && (!a_codes_dev || !a_scales_dev || !b_codes_dev || !b_scales_dev)) || (batch > 1 && batch_stride < (m - 1) * ld + n))
+    if (!out_dev || (length && (!a_codes_dev || !a_scales_dev || !b_codes_dev || !b_scales_dev)) || !mx4_apart(m, n, ld, batch, batch_stride))
         return KIMAD_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const MxProduct p{out_dev, ld, batch_stride, a_scales_dev, b_scales_dev, MxOperand((uint32_t)m, (uint32_t)length), MxOperand((uint32_t)n, (uint32_t)length),

@@ -6,7 +6,7 @@
 // scale is a normal number for every s in use, and what falls below the binary32 range then rounds to code 0 as it would have.
 // A block with Inf or NaN has s = 255 and codes 0.
 //   k_mx4_step       d = grad - g, C(d), g += C(d), ||d - C(d)||^2 (Eq. 4, Eq. 6 with this compressor)
-//   k_mx4_stats      the layers' errors and the workers' records from the CTAs' sums
+//   k_mx4_stats      the layers' errors and the workers' records, where the pass does not see to them
 //   k_mx4_apply      u^_m += C_m for every sender, and the model step (Algorithm 1, server lines)
 //   k_mx4_read       a message as dense values
 //   k_mx4_quantize_rows / _cols, k_mx4_dequantize_rows / _cols   operands (kimad_mx4_product.cuh multiplies them)
@@ -28,7 +28,7 @@ constexpr uint32_t kMxPer = 8;      // values of a lane: a warp has eight blocks
 constexpr uint32_t kMxGroup = 32 * kMxPer / kMxBlock, kMxGroupElems = 32 * kMxPer;
 constexpr int kMxWarps = kThreads / 32;
 
-struct MxPartial { // of a CTA of k_mx4_step
+struct __align__(16) MxPartial { // of a CTA of k_mx4_step
     double err;
     uint32_t absent, _pad;
 };
@@ -222,71 +222,36 @@ __device__ __forceinline__ void mx_step_group(const T* g, float* st, uint32_t li
     }
 }
 
-// One CTA per chunk, or per piece of one (1 << log_pieces of them) where the chunks are few; a warp takes eight blocks at a time.  Bound by HBM: 12.53
-// bytes per element with f32 gradients, 10.53 with 16-bit ones.  The difference d - C(d) is exact in binary32 (C(d) is zero or a multiple of half
-// a scale beside d), its squares are added in binary64: per lane, per CTA, per layer, always in the same order.
-// (A lane per element of a block, with the block's largest magnitude by a reduction over the warp, needs no vectors and no alignment but works
-// every scale out 32 times, 55 instructions per element: 4 x 124 M elements with bf16 gradients 1170 us, 847 this way.)
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-k_mx4_step(const T* __restrict__ grads, float* __restrict__ state, uint64_t stride, const Chunk* __restrict__ chunks,
-           const LayerDesc* __restrict__ layers, uint32_t log_pieces, MxMessage msg, MxPartial* __restrict__ partial) {
-    pdl_wait();
-    __shared__ __align__(16) float s_buf[kMxWarps][kMxGroupElems];
-    __shared__ double s_err[kMxWarps];
-    __shared__ uint32_t s_absent[kMxWarps];
-    const uint32_t w = blockIdx.y, f = blockIdx.x >> log_pieces, pieces = 1u << log_pieces, piece = blockIdx.x & (pieces - 1u);
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Chunk ch = chunks[f];
-    const MxSpan sp(ch, layers[ch.layer]);
-    const T* g = grads + (size_t)w * stride + sp.base;
-    float* st = state + (size_t)w * stride + sp.base;
-    uint32_t* words = msg.words(w, sp.first);
-    uint8_t* bytes = msg.bytes(w, sp.first);
-    const bool aligned = mx_aligned8(g) && mx_aligned8(st);
-    double err = 0.0;
-    uint32_t absent = 0;
-    for (uint32_t b = (piece * kMxWarps + warp) * kMxGroup; b < sp.blocks; b += pieces * kMxWarps * kMxGroup) {
-        const uint32_t e = b * kMxBlock, lim = min(sp.left - e, kMxGroupElems), blocks = min(sp.blocks - b, kMxGroup);
-        if (!KIMAD_CHECK((sp.first + b + blocks) * 16 <= msg.code_bytes && sp.first + b + blocks <= msg.scale_bytes, 8)) break;
-        if (aligned && lim == kMxGroupElems) mx_step_group<true>(g + e, st + e, lim, lane, blocks, words + b * 4, bytes + b, nullptr, err, absent);
-        else mx_step_group<false>(g + e, st + e, lim, lane, blocks, words + b * 4, bytes + b, s_buf[warp], err, absent);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) err += __shfl_xor_sync(0xffffffffu, err, o);
-    if (lane == 0) { s_err[warp] = err; s_absent[warp] = absent; }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        MxPartial p{0.0, 0, 0};
-        for (int i = 0; i < kMxWarps; ++i) { p.err += s_err[i]; p.absent += s_absent[i]; }
-        partial[(size_t)w * gridDim.x + blockIdx.x] = p;
-    }
-}
+// What becomes of the CTAs' sums: the layers' errors and the worker's record.
+struct MxStats {
+    MxPartial* partial; // [W][CTAs of a worker]
+    uint32_t* arrived;  // [W] CTAs that have left their sums, zero before and after; null where they are not counted
+    float* err;
+    kimad_stats* stats;
+    uint64_t n, message_bytes;
+    uint32_t L, check_finite;
+};
 
-// One CTA per worker.  The sums of a layer of few are added up by a thread, those of one of many by a warp, and by the CTA where a warp would
+// By one CTA for a worker.  The sums of a layer of few are added up by a thread, those of one of many by a warp, and by the CTA where a warp would
 // take long; the order depends on the layers only.  A layer with an absent block has an infinite error, as its difference has.
-constexpr int kMxStatsThreads = 1024;
-__global__ void __launch_bounds__(kMxStatsThreads)
-k_mx4_stats(const MxPartial* __restrict__ partial, const LayerDesc* __restrict__ layers, uint32_t L, uint32_t n_chunks, uint32_t log_pieces,
-            uint64_t n, uint64_t message_bytes, uint32_t check_finite, float* __restrict__ err, kimad_stats* __restrict__ stats) {
-    pdl_wait();
-    constexpr uint32_t kFew = 8, kMany = 512, kWarps = kMxStatsThreads / 32;
-    __shared__ double s_err[kWarps];
-    __shared__ uint32_t s_absent[kWarps];
-    const uint32_t w = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const MxPartial* mine = partial + ((size_t)w * n_chunks << log_pieces);
+template <uint32_t THREADS>
+__device__ __forceinline__ void mx_stats(const MxStats& st, const LayerDesc* layers, uint32_t w, uint32_t ctas, uint32_t log_pieces, double* s_err, uint32_t* s_absent) {
+    constexpr uint32_t WARPS = THREADS / 32;
+    constexpr uint32_t kFew = 8, kMany = 256;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const MxPartial* mine = st.partial + (size_t)w * ctas;
     double total = 0.0;
     uint32_t absent = 0;
     auto add = [&](const LayerDesc& ld, uint32_t from, uint32_t step, double& sum, uint32_t& gone) {
-        const MxPartial* at = mine + ((size_t)ld.first_chunk << log_pieces);
+        const uint4* at = reinterpret_cast<const uint4*>(mine + ((size_t)ld.first_chunk << log_pieces));
         const uint32_t count = ld.n_chunks << log_pieces;
         sum = 0.0;
         gone = 0;
 #pragma unroll 4
         for (uint32_t i = from; i < count; i += step) {
-            const MxPartial p = at[i];
-            sum += p.err;
-            gone += p.absent;
+            const uint4 p = __ldcg(at + i); // written by other CTAs of this kernel
+            sum += __hiloint2double((int)p.y, (int)p.x);
+            gone += p.z;
         }
     };
     auto over_warp = [&](double& sum, uint32_t& gone) {
@@ -301,20 +266,17 @@ k_mx4_stats(const MxPartial* __restrict__ partial, const LayerDesc* __restrict__
         __syncthreads();
         if (lane == 0) { s_err[warp] = sum; s_absent[warp] = gone; }
         __syncthreads();
-        if (warp == 0) {
-            sum = s_err[lane];
-            gone = s_absent[lane];
-            over_warp(sum, gone);
-        }
+        if (threadIdx.x == 0)
+            for (uint32_t i = 1; i < WARPS; ++i) { sum += s_err[i]; gone += s_absent[i]; }
     };
     auto done = [&](uint32_t l, double sum, uint32_t gone) {
         if (gone) sum = (double)__int_as_float(0x7f800000);
-        err[(size_t)w * L + l] = (float)sum;
+        st.err[(size_t)w * st.L + l] = (float)sum;
         total += sum;
         absent += gone;
     };
     uint32_t many = 0;
-    for (uint32_t l = threadIdx.x; l < L; l += kMxStatsThreads) {
+    for (uint32_t l = threadIdx.x; l < st.L; l += THREADS) {
         const LayerDesc ld = layers[l];
         const uint32_t count = ld.n_chunks << log_pieces;
         many += count > kMany;
@@ -324,7 +286,7 @@ k_mx4_stats(const MxPartial* __restrict__ partial, const LayerDesc* __restrict__
         add(ld, 0, 1, sum, gone);
         done(l, sum, gone);
     }
-    for (uint32_t l = warp; l < L; l += kWarps) {
+    for (uint32_t l = warp; l < st.L; l += WARPS) {
         const LayerDesc ld = layers[l];
         const uint32_t count = ld.n_chunks << log_pieces;
         if (count <= kFew || count > kMany) continue;
@@ -335,24 +297,84 @@ k_mx4_stats(const MxPartial* __restrict__ partial, const LayerDesc* __restrict__
         if (lane == 0) done(l, sum, gone);
     }
     if (__syncthreads_or(many))
-        for (uint32_t l = 0; l < L; ++l) {
+        for (uint32_t l = 0; l < st.L; ++l) {
             const LayerDesc ld = layers[l];
             if (ld.n_chunks << log_pieces <= kMany) continue;
             double sum;
             uint32_t gone;
-            add(ld, threadIdx.x, kMxStatsThreads, sum, gone);
+            add(ld, threadIdx.x, THREADS, sum, gone);
             over_cta(sum, gone);
             if (threadIdx.x == 0) done(l, sum, gone);
         }
     over_cta(total, absent);
     if (threadIdx.x == 0) {
         kimad_stats s{};
-        s.used_bytes = message_bytes;
-        s.n_selected = n;
+        s.used_bytes = st.message_bytes;
+        s.n_selected = st.n;
         s.total_err = (float)total;
-        s.status = absent && check_finite ? KIMAD_ERR_NONFINITE : KIMAD_OK;
-        stats[w] = s;
+        s.status = absent && st.check_finite ? KIMAD_ERR_NONFINITE : KIMAD_OK;
+        st.stats[w] = s;
     }
+}
+
+// Where the CTAs are few, the last one of a worker does that: the pass of a small model then is one launch (0.10 M elements: 4.5 us of the host's time instead of
+// 6.3).  Where they are many, a kernel of its own behind them: their arrivals and the smaller CTA cost more there (2 x 25.6 M elements 285 us instead of 277).
+constexpr uint32_t kMxStatsThreads = 1024;
+__global__ void __launch_bounds__(kMxStatsThreads)
+k_mx4_stats(MxStats st, const LayerDesc* __restrict__ layers, uint32_t ctas, uint32_t log_pieces) {
+    pdl_wait();
+    __shared__ double s_err[kMxStatsThreads / 32];
+    __shared__ uint32_t s_absent[kMxStatsThreads / 32];
+    mx_stats<kMxStatsThreads>(st, layers, blockIdx.x, ctas, log_pieces, s_err, s_absent);
+}
+
+// One CTA per chunk, or per piece of one (1 << log_pieces of them) where the chunks are few; a warp takes eight blocks at a time.  Bound by HBM: 12.53
+// bytes per element with f32 gradients, 10.53 with 16-bit ones.  The difference d - C(d) is exact in binary32 (C(d) is zero or a multiple of half
+// a scale beside d), its squares are added in binary64: per lane, per CTA, per layer, always in the same order.
+// (A lane per element of a block, with the block's largest magnitude by a reduction over the warp, needs no vectors and no alignment but works
+// every scale out 32 times, 55 instructions per element: 4 x 124 M elements with bf16 gradients 1170 us, 839 this way.)
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+k_mx4_step(const T* __restrict__ grads, float* __restrict__ state, uint64_t stride, const Chunk* __restrict__ chunks,
+           const LayerDesc* __restrict__ layers, uint32_t log_pieces, MxMessage msg, MxStats st) {
+    pdl_wait();
+    __shared__ __align__(16) float s_buf[kMxWarps][kMxGroupElems];
+    __shared__ double s_err[kMxWarps];
+    __shared__ uint32_t s_absent[kMxWarps], s_last;
+    const uint32_t w = blockIdx.y, f = blockIdx.x >> log_pieces, pieces = 1u << log_pieces, piece = blockIdx.x & (pieces - 1u);
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Chunk ch = chunks[f];
+    const MxSpan sp(ch, layers[ch.layer]);
+    const T* g = grads + (size_t)w * stride + sp.base;
+    float* at = state + (size_t)w * stride + sp.base;
+    uint32_t* words = msg.words(w, sp.first);
+    uint8_t* bytes = msg.bytes(w, sp.first);
+    const bool aligned = mx_aligned8(g) && mx_aligned8(at);
+    double err = 0.0;
+    uint32_t absent = 0;
+    for (uint32_t b = (piece * kMxWarps + warp) * kMxGroup; b < sp.blocks; b += pieces * kMxWarps * kMxGroup) {
+        const uint32_t e = b * kMxBlock, lim = min(sp.left - e, kMxGroupElems), blocks = min(sp.blocks - b, kMxGroup);
+        if (!KIMAD_CHECK((sp.first + b + blocks) * 16 <= msg.code_bytes && sp.first + b + blocks <= msg.scale_bytes, 8)) break;
+        if (aligned && lim == kMxGroupElems) mx_step_group<true>(g + e, at + e, lim, lane, blocks, words + b * 4, bytes + b, nullptr, err, absent);
+        else mx_step_group<false>(g + e, at + e, lim, lane, blocks, words + b * 4, bytes + b, s_buf[warp], err, absent);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) err += __shfl_xor_sync(0xffffffffu, err, o);
+    if (lane == 0) { s_err[warp] = err; s_absent[warp] = absent; }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        MxPartial p{0.0, 0, 0};
+        for (int i = 0; i < kMxWarps; ++i) { p.err += s_err[i]; p.absent += s_absent[i]; }
+        st.partial[(size_t)w * gridDim.x + blockIdx.x] = p;
+        if (st.arrived) {
+            __threadfence();
+            s_last = atomicInc(st.arrived + w, gridDim.x - 1) == gridDim.x - 1; // back to zero with the last one
+            __threadfence();
+        }
+    }
+    if (!st.arrived) return;
+    __syncthreads();
+    if (s_last) mx_stats<kThreads>(st, layers, w, gridDim.x, log_pieces, s_err, s_absent);
 }
 
 // Eight blocks of a message in a warp: a lane's eight values (0 where the block is absent); the lanes of absent blocks come back as a mask.

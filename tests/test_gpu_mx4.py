@@ -21,6 +21,7 @@ LAYERS = {
     "edges": [1, 31, 32, 33, 255, 256, 257, 7, 64],
     "chunks": [5, 32768 * 2 + 5, 100, 40000, 32640, 1],
     "many": [3] * 700 + [64] * 200,
+    "large": [40000 * 257, 9, 32768 * 300, 33] + [40000] * 40 + [100] * 900,  # more than 1184 chunks: the errors by a kernel of their own
 }
 
 
@@ -86,7 +87,7 @@ class Case:
 
 @pytest.mark.parametrize("layers,W,pad,dtype,shift", [
     ("one", 1, 0, "f32", 0), ("one", 3, 1, "bf16", 1), ("edges", 1, 0, "f32", 0), ("edges", 2, 0, "f32", 1), ("edges", 3, 5, "f16", 3),
-    ("chunks", 1, 0, "f32", 0), ("chunks", 2, 0, "bf16", 0), ("chunks", 2, 3, "f32", 2), ("many", 2, 0, "f32", 0), ("many", 1, 0, "f16", 1)])
+    ("chunks", 1, 0, "f32", 0), ("chunks", 2, 0, "bf16", 0), ("chunks", 2, 3, "f32", 2), ("many", 2, 0, "f32", 0), ("many", 1, 0, "f16", 1), ("large", 1, 1, "bf16", 1)])
 def test_step_matches_the_definition(layers, W, pad, dtype, shift):
     c = Case(LAYERS[layers], W, pad, dtype, shift)
     for _ in range(2):  # the second one starts from what the first one left
@@ -204,7 +205,7 @@ def test_both_kinds_of_steps_share_a_context():
         launches = kb.kimad_launch_count(r.ctx)
         kb.kimad_mx4_step(r.ctx, grads, state, msg)
         torch.cuda.synchronize()
-        assert kb.kimad_launch_count(r.ctx) == launches + 2
+        assert kb.kimad_launch_count(r.ctx) == launches + 1
         for w in range(wl.n_workers):
             c, sc, *_ = _mx4.message(g[w], wl.layer_sizes)
             assert np.array_equal(msg.codes[w].cpu().numpy(), c) and np.array_equal(msg.scales[w, :len(sc)].cpu().numpy(), sc)

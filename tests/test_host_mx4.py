@@ -113,7 +113,7 @@ def test_quantize_and_dequantize_refusals():
         assert L.kimad_mx4_quantize(*a) == kb.KIMAD_OK
     # codes, scales, x, dtype, rows, cols, ld, batch, batch_stride, along, stream
     good = [512, 1024, 256, 0, 5, 7, 8, 2, 39, 1, None]
-    for i, v in [(0, None), (0, 520), (1, None), (2, None), (2, 257), (3, 2), (6, 6), (8, 38), (9, 2)]:
+    for i, v in [(0, None), (0, 520), (1, None), (2, None), (2, 257), (3, 2), (6, 6), (6, 1 << 62), (8, 38), (9, 2)]:  # (4 * 2^62 is no distance in 64 bits)
         a = list(good)
         a[i] = v
         assert L.kimad_mx4_dequantize(*a) == BAD, (i, v)
