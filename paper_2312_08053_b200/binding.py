@@ -455,14 +455,15 @@ def _mx4_dtype(t, what, most=KIMAD_F16):
     return code
 
 
-def _mx4_stream(what, stream, *devices):
-    """The library takes memory of the current device: a tensor of another one is refused, as is one in host memory (device -1)."""
-    if min(devices) < 0:
-        raise ValueError(f"{what}: a tensor in host memory")
-    here = _mx4_device()
-    for d in devices:
+def _mx4_stream(what, stream, here, *others):
+    """The stream's handle.  The library takes memory of the current device: a tensor of another one is refused, as is one in host memory (device -1)."""
+    for d in others:
         if d != here:
-            raise ValueError(f"{what}: a tensor on cuda:{d}, the current device is cuda:{here}")
+            raise ValueError(f"{what}: tensors on different devices")
+    if here < 0:
+        raise ValueError(f"{what}: a tensor in host memory")
+    if here != _mx4_device():
+        raise ValueError(f"{what}: a tensor on cuda:{here}, the current device is cuda:{_mx4_device()}")
     return _mx4_raw_stream(here) if stream is None else _stream_ptr(stream)
 
 
@@ -574,14 +575,15 @@ class Mx4Operand:
         if self.codes.get_device() != self.scales.get_device():
             raise ValueError("an operand's codes and scales are on one device")
         self.device = self.codes.get_device()
+        self.shapes = ((self.batch, self.length, self.lines), (self.batch, self.lines, self.length))  # of the matrix, by `along`
         self.codes_ptr, self.scales_ptr = self.codes.data_ptr(), self.scales.data_ptr()
 
 
-def _mx4_matrix(t, batch, rows, cols, what):
-    """(row stride, matrix stride) of a [rows][cols] or [batch][rows][cols] tensor."""
+def _mx4_matrix(t, shape, what):
+    """(row stride, matrix stride) of a [rows][cols] or [batch][rows][cols] tensor of this shape."""
+    batch, rows, cols = shape
     stride = t.stride()
-    shape = t.shape if len(stride) == 3 else (1, *t.shape)
-    if shape != (batch, rows, cols):
+    if (t.shape if len(stride) == 3 else (1, *t.shape)) != shape:
         raise ValueError(f"{what}: {tuple(t.shape)} does not go with an operand, {batch} x {rows} x {cols} does")
     ld = stride[-2] if rows > 1 else cols
     if (cols > 1 and stride[-1] != 1) or ld < cols:
@@ -592,27 +594,27 @@ def _mx4_matrix(t, batch, rows, cols, what):
 def _mx4_along(op, along):
     if along not in (0, 1):
         raise ValueError("along: 0, blocks over the rows, or 1, over the columns")
-    return (op.length, op.lines) if along == 0 else (op.lines, op.length)
+    return op.shapes[along]
 
 
 def kimad_mx4_quantize(x, op: Mx4Operand, along: int, stream=None) -> None:
     """x: CUDA float32, bfloat16 or float16, [rows][cols] or [batch][rows][cols].  along 0: blocks over the rows (the operand is x transposed), 1: over
     the columns."""
     dtype = _mx4_dtype(x, "x")
-    rows, cols = _mx4_along(op, along)
-    ld, bs = _mx4_matrix(x, op.batch, rows, cols, "x")
+    shape = _mx4_along(op, along)
+    ld, bs = _mx4_matrix(x, shape, "x")
     s = _mx4_stream("kimad_mx4_quantize", stream, x.get_device(), op.device)
-    _check((_lib or load()).kimad_mx4_quantize(x.data_ptr(), dtype, rows, cols, ld, op.batch, bs, along, op.codes_ptr, op.scales_ptr, s),
+    _check((_lib or load()).kimad_mx4_quantize(x.data_ptr(), dtype, shape[1], shape[2], ld, shape[0], bs, along, op.codes_ptr, op.scales_ptr, s),
            "kimad_mx4_quantize")
 
 
 def kimad_mx4_dequantize(op: Mx4Operand, out, along: int, stream=None) -> None:
     """out: CUDA float32 or bfloat16, shaped as kimad_mx4_quantize's x."""
     dtype = _mx4_dtype(out, "out", KIMAD_BF16)
-    rows, cols = _mx4_along(op, along)
-    ld, bs = _mx4_matrix(out, op.batch, rows, cols, "out")
+    shape = _mx4_along(op, along)
+    ld, bs = _mx4_matrix(out, shape, "out")
     s = _mx4_stream("kimad_mx4_dequantize", stream, out.get_device(), op.device)
-    _check((_lib or load()).kimad_mx4_dequantize(op.codes_ptr, op.scales_ptr, out.data_ptr(), dtype, rows, cols, ld, op.batch, bs, along, s),
+    _check((_lib or load()).kimad_mx4_dequantize(op.codes_ptr, op.scales_ptr, out.data_ptr(), dtype, shape[1], shape[2], ld, shape[0], bs, along, s),
            "kimad_mx4_dequantize")
 
 
@@ -622,7 +624,7 @@ def kimad_mx4_product(a: Mx4Operand, b: Mx4Operand, out, alpha=1.0, beta=0.0, st
     _mx4_dtype(out, "out", KIMAD_F32)
     if a.length != b.length or a.batch != b.batch:
         raise ValueError(f"kimad_mx4_product: operands of {a.batch} x {a.length} and of {b.batch} x {b.length}")
-    ld, bs = _mx4_matrix(out, a.batch, a.lines, b.lines, "out")
+    ld, bs = _mx4_matrix(out, (a.batch, a.lines, b.lines), "out")
     s = _mx4_stream("kimad_mx4_product", stream, out.get_device(), a.device, b.device)
     if status is not None:
         if str(status.dtype) != "torch.int32" or status.numel() < 1:
