@@ -467,6 +467,11 @@ def _mx4_stream(what, stream, here, *others):
     return _mx4_raw_stream(here) if stream is None else _stream_ptr(stream)
 
 
+def _mx4_home(ctx, here):
+    """The device of the context's workspace, which the kernels read (`here` where none is attached: the library refuses that)."""
+    return ctx._keep[0].get_device() if ctx._keep else here
+
+
 def _mx4_workers(ctx, t, what):
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or shape[0] != ctx.W or shape[1] < ctx.N or (shape[1] > 1 and stride[1] != 1) or (ctx.W > 1 and stride[0] != ctx.stride):
@@ -521,7 +526,7 @@ def kimad_mx4_step(ctx: Ctx, grads, state, msg: Mx4Message, stream=None) -> None
     _mx4_workers(ctx, grads, "grads")
     _mx4_workers(ctx, state, "state")
     m = _mx4_message(ctx, msg, "kimad_mx4_step")
-    s = _mx4_stream("kimad_mx4_step", stream, grads.get_device(), state.get_device(), msg.device)
+    s = _mx4_stream("kimad_mx4_step", stream, here := grads.get_device(), state.get_device(), msg.device, _mx4_home(ctx, here))
     _check((_lib or load()).kimad_mx4_step(ctx.handle, grads.data_ptr(), dtype, state.data_ptr(), m, s), "kimad_mx4_step")
 
 
@@ -531,14 +536,14 @@ def kimad_mx4_apply(ctx: Ctx, msg: Mx4Message, est, x=None, weights=None, gamma=
     _mx4_workers(ctx, est, "est")
     m = _mx4_message(ctx, msg, "kimad_mx4_apply")
     if x is None:
-        s = _mx4_stream("kimad_mx4_apply", stream, est.get_device(), msg.device)
+        s = _mx4_stream("kimad_mx4_apply", stream, here := est.get_device(), msg.device, _mx4_home(ctx, here))
         _check((_lib or load()).kimad_mx4_apply(ctx.handle, m, est.data_ptr(), None, None, 0.0, s), "kimad_mx4_apply")
         return
     _mx4_dtype(x, "x", KIMAD_F32)
     w = np.ascontiguousarray([] if weights is None else weights, dtype=np.float32).reshape(-1)
     if w.size != ctx.W or x.dim() != 1 or x.numel() != ctx.N or (ctx.N > 1 and x.stride(0) != 1):
         raise ValueError(f"kimad_mx4_apply: x of {ctx.N} consecutive elements and {ctx.W} weights")
-    s = _mx4_stream("kimad_mx4_apply", stream, est.get_device(), x.get_device(), msg.device)
+    s = _mx4_stream("kimad_mx4_apply", stream, here := est.get_device(), x.get_device(), msg.device, _mx4_home(ctx, here))
     _check((_lib or load()).kimad_mx4_apply(ctx.handle, m, est.data_ptr(), x.data_ptr(), w.ctypes.data_as(C.POINTER(C.c_float)), gamma, s), "kimad_mx4_apply")
 
 
@@ -547,7 +552,7 @@ def kimad_mx4_read(ctx: Ctx, msg: Mx4Message, out, stream=None) -> None:
     dtype = _mx4_dtype(out, "out", KIMAD_BF16)
     _mx4_workers(ctx, out, "out")
     m = _mx4_message(ctx, msg, "kimad_mx4_read")
-    s = _mx4_stream("kimad_mx4_read", stream, out.get_device(), msg.device)
+    s = _mx4_stream("kimad_mx4_read", stream, here := out.get_device(), msg.device, _mx4_home(ctx, here))
     _check((_lib or load()).kimad_mx4_read(ctx.handle, m, out.data_ptr(), dtype, s), "kimad_mx4_read")
 
 

@@ -156,6 +156,23 @@ def test_binding_refuses_shapes_types_and_places():
         kb.Mx4Operand(7, 5, codes=torch.zeros(6, dtype=torch.uint8), scales=torch.zeros(512, dtype=torch.uint8))
 
 
+def test_binding_refuses_a_workspace_of_another_device():
+    import torch
+
+    class Elsewhere:
+        def get_device(self):
+            return 1
+
+    ctx = _ctx((40, 8), W=2)
+    msg = kb.Mx4Message(ctx, device="cpu")
+    t, x = torch.zeros((2, 48)), torch.zeros(48)
+    ctx._keep = [Elsewhere()]
+    for call in (lambda: kb.kimad_mx4_step(ctx, t, t.clone(), msg), lambda: kb.kimad_mx4_apply(ctx, msg, t),
+                 lambda: kb.kimad_mx4_apply(ctx, msg, t, x, [0.5, 0.5], 0.1), lambda: kb.kimad_mx4_read(ctx, msg, t)):
+        with pytest.raises(ValueError, match="different devices"):
+            call()
+
+
 def test_product_refusals():
     L = kb.load()
     # out, ld, batch_stride, m, n, length, batch, a codes, a scales, b codes, b scales, alpha, beta, status, stream
