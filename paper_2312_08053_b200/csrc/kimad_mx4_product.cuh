@@ -42,23 +42,35 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
+// ... for a phase that another CTA of the cluster arrives in.
+__device__ __forceinline__ bool mbar_try_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
 // Waits of whole warps, bounded: false, for all lanes, when the phase has not ended within the limit or another warp of the CTA has given up.
 struct MxWait {
     volatile uint32_t* flag;
     long long clocks;
     __device__ __forceinline__ bool failed() const { return __any_sync(0xffffffffu, *flag != 0); }
 };
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const MxWait& w) {
-    bool ended = mbar_try(bar, parity);
+template <bool CLUSTER = false> __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const MxWait& w) {
+    auto look = [&] { return CLUSTER ? mbar_try_cluster(bar, parity) : mbar_try(bar, parity); };
+    bool ended = look();
     if (__all_sync(0xffffffffu, ended)) return true;
     const long long began = clock64();
-    while (!ended && !(ended = mbar_try(bar, parity)))
+    while (!ended && !(ended = look()))
         if (*w.flag || clock64() - began > w.clocks) { *w.flag = 1; break; }
     return __all_sync(0xffffffffu, ended);
 }
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x),
+                 "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// A load into this CTA's shared memory that is counted on a barrier of either CTA of its pair.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x),
                  "r"(y), "r"(z), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -453,8 +465,10 @@ constexpr int kMxPairThreads = 480;
 constexpr uint32_t kMxPairScaleCols = 24; // of a stage: A's 2 x 4, B's 2 x 8 (6 in use)
 static_assert(kMxPairStageBytes % 1024 == 0 && kMxPairN == 192, "shared memory; tc_store_scales");
 
-// Arrival on the barrier of the pair's first CTA.  Relaxed: what is handed over are accesses to tensor memory that have been waited for (tcgen05.wait) and
-// copies that have been, none of the thread's own writes; with release the arrival waits for every store under way, about 1000 clocks.
+// Arrival on the barrier of the pair's first CTA, for accesses to tensor memory and nothing else: they have been waited for (tcgen05.wait), and
+// tcgen05.fence before the arrival and behind the other side's wait orders them, so that the arrival itself may be relaxed.  (With release it waits for every
+// store under way, about 1000 clocks.)  The codes, which the copy engine writes to either CTA's shared memory, are counted on the first CTA's barrier
+// themselves.
 __device__ __forceinline__ void mbar_arrive_first(uint32_t bar) {
     asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %0, 0;\nmbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [a];\n}" ::"r"(bar) : "memory");
 }
@@ -487,15 +501,15 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     const __grid_constant__ MxProduct p, uint32_t all_tiles, uint32_t by_tma) {
     extern __shared__ uint8_t smem_raw[];
     static_assert(2 * kMxPairN + S * kMxPairScaleCols <= 512 && mx_pair_smem(S, SLABS) <= 227 * 1024 && SLABS <= kMxPairN / 64, "tensor memory, shared memory");
-    __shared__ __align__(8) uint64_t s_bar[3 * S + 5 + 8 * SLABS];
+    __shared__ __align__(8) uint64_t s_bar[4 * S + 5 + 8 * SLABS];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_failed;
     const MxWait wait{&s_failed, p.wait_clocks};
     const uint32_t warp = warp_number(), lane = threadIdx.x & 31, rank = cluster_rank();
     const uint32_t bar = smem_u32(s_bar), smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    // a stage's copies are here; its scales are in tensor memory, in both CTAs (first CTA); its products are done; a tile's products are done; its sums
-    // have been read, in both CTAs (first CTA); everything issued is done
-    const uint32_t full = bar, ready = bar + 8 * S, empty = bar + 16 * S, done = bar + 24 * S, drained = done + 16, quit = done + 32,
+    // a stage's scales are here; its codes are, in both CTAs (first CTA); its scales are in tensor memory, in both CTAs (first CTA); its products are done; a
+    // tile's products are done; its sums have been read, in both CTAs (first CTA); everything issued is done
+    const uint32_t full = bar, codes = bar + 8 * S, ready = bar + 16 * S, empty = bar + 24 * S, done = bar + 32 * S, drained = done + 16, quit = done + 32,
                    old = quit + 8; // (an output warp's slabs of old values, SLABS each)
     if (warp == 12 && one_lane()) {
         tma_prefetch(&map_a);
@@ -503,7 +517,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         if (by_tma) tma_prefetch(&map_out);
     }
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 2); mbar_init(ready + 8 * s, 8); mbar_init(empty + 8 * s, 1); }
+        for (uint32_t s = 0; s < S; ++s) { mbar_init(full + 8 * s, 1); mbar_init(codes + 8 * s, 1); mbar_init(ready + 8 * s, 8); mbar_init(empty + 8 * s, 1); }
         for (uint32_t b = 0; b < 2; ++b) { mbar_init(done + 8 * b, 1); mbar_init(drained + 8 * b, 16); }
         mbar_init(quit, 1);
         for (uint32_t i = 0; i < 8 * SLABS; ++i) mbar_init(old + 8 * i, 1);
@@ -526,15 +540,16 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     uint32_t it = 0; // stages whose copies, or whose products, have been issued
     MxRing<S> q;
     if (warp == 12) {
+        const uint32_t counted = shared_of(codes, 0);
         for (uint32_t tile = pair; tile < all_tiles && !p.withhold && !wait.failed(); tile += pairs) {
             const MxPairTile t(p, tile);
             for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
-                const uint32_t to = smem + q.s * kMxPairStageBytes, here = full + 8 * q.s;
+                const uint32_t to = smem + q.s * kMxPairStageBytes, there = counted + 8 * q.s;
                 if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, wait)) break;
-                if (one_lane()) {
-                    mbar_expect(here, kMxOperandStage + kMxPairBytesB);
-                    tma_load_3d(to, &map_a, (int)(r * 128), (int)(t.row + rank * kMxTile), (int)t.n, here);
-                    tma_load_3d(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(t.col + rank * (kMxPairN / 2)), (int)t.n, here);
+                if (one_lane()) { // (the second CTA's bytes may arrive before they are expected: the phase does not end before the first CTA's arrival)
+                    if (rank == 0) mbar_expect(codes + 8 * q.s, 2 * (kMxOperandStage + kMxPairBytesB));
+                    tma_load_3d_pair(to, &map_a, (int)(r * 128), (int)(t.row + rank * kMxTile), (int)t.n, there);
+                    tma_load_3d_pair(to + kMxOperandStage, &map_b, (int)(r * 128), (int)(t.col + rank * (kMxPairN / 2)), (int)t.n, there);
                 }
             }
         }
@@ -562,12 +577,12 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         uint32_t j = 0; // tiles of this pair
         for (uint32_t tile = pair; tile < all_tiles && !wait.failed(); tile += pairs, ++j, u.next()) {
             const uint32_t sums = tmem + u.s * kMxPairN;
-            if (j >= 2 && !mbar_wait(drained + 8 * u.s, u.parity ^ 1u, wait)) break;
+            if (j >= 2 && !mbar_wait<true>(drained + 8 * u.s, u.parity ^ 1u, wait)) break;
             for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
                 const uint32_t scales = tmem + 2 * kMxPairN + kMxPairScaleCols * q.s;
                 const uint64_t a = mx_desc_codes(smem + q.s * kMxPairStageBytes), b = mx_desc_codes(smem + q.s * kMxPairStageBytes + kMxOperandStage);
                 const uint32_t products = min((p.a.blocks - r * 8 + 1) / 2, 4u); // of 64 values, two blocks, each
-                if (!mbar_wait(ready + 8 * q.s, q.parity, wait)) break;
+                if (!mbar_wait(codes + 8 * q.s, q.parity, wait) || !mbar_wait<true>(ready + 8 * q.s, q.parity, wait)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (one_lane()) {
 #pragma unroll
@@ -691,7 +706,10 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (s_failed) { // what was issued still writes to the pair's shared and tensor memory
         if (threadIdx.x == 0 && p.status) *p.status = KIMAD_ERR_TIMEOUT;
         const long long began = clock64();
-        if ((warp == 12 || warp == 14) && lane == 0) // (a stage of which only one of them has issued its copies does not end, but they do within the limit)
+        if (warp == 12 && lane == 0 && rank == 0) // (the second CTA may be S stages ahead; a stage that only one has issued does not end, but its copies do within the limit)
+            for (uint32_t i = it > S ? it - S : 0; i < it + S && !p.withhold; ++i)
+                while (!mbar_try(codes + 8 * (i % S), (i / S) & 1u) && clock64() - began < kMxWaitClocks) {}
+        if (warp == 14 && lane == 0)
             for (uint32_t i = it > S ? it - S : 0; i < it; ++i)
                 while (!mbar_try(full + 8 * (i % S), (i / S) & 1u) && clock64() - began < kMxWaitClocks) {}
         if (warp == 13 && lane == 0 && rank == 0)
