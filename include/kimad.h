@@ -240,8 +240,8 @@ int kimad_aggregate(float* x_dev, const float* est_dev, uint64_t stride, uint32_
  * about an eighth of the dense f32 bytes: whether it fits a budget is known without a search (compare with kimad_plan_budget's c).
  * Device memory of the caller's, all workers behind each other:
  *   codes   u8 [W][code_bytes], scales u8 [W][scale_bytes]  both 16-byte aligned
- *   err     f32 [W][L]  ||d_l - C(d_l)||^2, summed in binary64; may be NULL where the message is only read
- *   stats   [W]         used_bytes = 17 bytes per block, n_selected = N, budget_bytes = 0 (no budget is taken); may be NULL likewise
+ *   err     f32 [W][L]  ||d_l - C(d_l)||^2, summed in binary64; 4-byte aligned; may be NULL where the message is only read
+ *   stats   [W]         used_bytes = 17 bytes per block, n_selected = N, budget_bytes = 0 (no budget is taken); 8-byte aligned; may be NULL likewise
  * The same contexts as for TopK, of any policy (at most 65535 workers), with their workspace attached; the ratio grid and D play no role.
  * Steps of either kind may follow each other on the same estimators. */
 enum { KIMAD_F32 = 0, KIMAD_BF16 = 1, KIMAD_F16 = 2 }; /* element types of the calls below */

@@ -1193,7 +1193,7 @@ int kimad_mx4_message_bytes(const kimad_ctx* c, uint64_t* code_bytes, uint64_t* 
 }
 
 int kimad_mx4_step(kimad_ctx* c, const void* grads_dev, uint32_t grad_dtype, float* state_dev, const kimad_mx4_message* out, void* cuda_stream) {
-    if (!mx4_message_ok(c, out) || !out->err || !out->stats || !grads_dev || !state_dev || grad_dtype > KIMAD_F16 ||
+    if (!mx4_message_ok(c, out) || !out->err || (uintptr_t)out->err % alignof(float) || !out->stats || (uintptr_t)out->stats % alignof(kimad_stats) || !grads_dev || !state_dev || grad_dtype > KIMAD_F16 ||
         (uintptr_t)grads_dev % (grad_dtype == KIMAD_F32 ? 4 : 2) || (uintptr_t)state_dev % 4)
         return KIMAD_ERR_INVALID_ARG;
     if (!c->ws) return KIMAD_ERR_WORKSPACE;
