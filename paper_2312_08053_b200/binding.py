@@ -182,6 +182,7 @@ class Ctx:
         self.value_dtype = opts.value_dtype
         self.cap = opts.max_packed_elems or N
         self.stride = opts.worker_stride or N
+        self.layer_sizes = b""  # u64 [L], as bytes
         self._keep = []  # tensors the context points into (workspace)
 
     def __del__(self):
@@ -198,7 +199,9 @@ def kimad_create(layer_sizes, n_workers, ratio_grid, D=0, value_dtype=0, check_f
     h = C.c_void_p()
     _check(load().kimad_create(C.byref(h), ls.ctypes.data_as(C.POINTER(C.c_uint64)), ls.size, n_workers,
                                rg.ctypes.data_as(C.POINTER(C.c_double)), rg.size, C.byref(opts)), "kimad_create")
-    return Ctx(h, int(ls.size), int(n_workers), int(rg.size), int(ls.sum()), opts)
+    ctx = Ctx(h, int(ls.size), int(n_workers), int(rg.size), int(ls.sum()), opts)
+    ctx.layer_sizes = ls.tobytes()
+    return ctx
 
 
 def kimad_destroy(ctx: Ctx) -> None:
@@ -486,10 +489,10 @@ def kimad_mx4_message_bytes(ctx: Ctx):
 
 
 def _mx4_shape(ctx):
-    """What two contexts share that can read each other's messages."""
+    """What two contexts share that can read each other's messages: the workers and the layers' sizes, which decide where blocks begin."""
     shape = getattr(ctx, "_mx4_shape", None)
     if shape is None:
-        shape = ctx._mx4_shape = (ctx.W, ctx.L, *kimad_mx4_message_bytes(ctx))
+        shape = ctx._mx4_shape = (ctx.W, ctx.L, *kimad_mx4_message_bytes(ctx), ctx.layer_sizes)
     return shape
 
 
@@ -500,7 +503,7 @@ class Mx4Message:
         import torch
 
         self.shape = _mx4_shape(ctx)
-        W, L, code_bytes, scale_bytes = self.shape
+        W, L, code_bytes, scale_bytes, _ = self.shape
         self.codes = torch.zeros((W, code_bytes), dtype=torch.uint8, device=device)
         self.scales = torch.zeros((W, scale_bytes), dtype=torch.uint8, device=device)
         self.err = torch.zeros((W, L), dtype=torch.float32, device=device)
@@ -514,7 +517,8 @@ class Mx4Message:
 
 
 def _mx4_message(ctx, msg, what):
-    if msg.shape != _mx4_shape(ctx):
+    shape = _mx4_shape(ctx)
+    if msg.shape is not shape and msg.shape != shape:
         raise ValueError(f"{what}: a message of another context's shape")
     return msg.ref
 

@@ -24,3 +24,26 @@ def test_step_refuses_errors_and_statistics_that_are_not_aligned(err, stats):
 
     assert call(260, 264) == kb.KIMAD_ERR_WORKSPACE  # everything is right but the workspace, which comes last
     assert call(err, stats) == BAD
+
+
+@pytest.mark.parametrize("layers", [[40, 33], [33, 41], [33, 64]])
+def test_messages_of_contexts_with_other_layers_are_refused(layers):
+    """The blocks of [33, 40] are those of these contexts in number, not in place."""
+    import torch
+
+    of, to = kb.kimad_create([33, 40], 2, [1.0]), kb.kimad_create(layers, 2, [1.0])
+    assert kb.kimad_mx4_message_bytes(of) == kb.kimad_mx4_message_bytes(to)
+    msg, t = kb.Mx4Message(of, device="cpu"), torch.zeros((2, sum(layers)))
+    for call in (lambda: kb.kimad_mx4_step(to, t, t.clone(), msg), lambda: kb.kimad_mx4_apply(to, msg, t), lambda: kb.kimad_mx4_read(to, msg, t)):
+        with pytest.raises(ValueError, match="another context's shape"):
+            call()
+
+
+def test_messages_of_contexts_with_the_same_layers_are_taken():
+    """Whatever else the contexts differ in.  (What is refused here is a tensor in host memory.)"""
+    import torch
+
+    of, to = kb.kimad_create([33, 40], 2, [1.0]), kb.kimad_create([33, 40], 2, [0.1, 1.0], worker_stride=80, policy=1)
+    msg = kb.Mx4Message(of, device="cpu")
+    with pytest.raises(ValueError, match="host memory"):
+        kb.kimad_mx4_read(to, msg, torch.zeros((2, 80)))
