@@ -1147,6 +1147,15 @@ EncodeTiled encode_tiled() {
     return f;
 }
 
+// The driver's call wants a current context, which a thread that has made no runtime call that needs one does not have yet: it gets its device's then.
+template <typename... Args> bool encode_map(Args... args) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    if (encode(args...) == CUDA_SUCCESS) return true;
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode(args...) == CUDA_SUCCESS;
+}
+
 // The product's shared memory is above the default limit, which is raised once on every device.
 int mx4_prepare_product() {
     static std::atomic<uint64_t> raised[4] = {};
@@ -1167,9 +1176,8 @@ int mx4_prepare_product() {
 bool mx4_map(CUtensorMap* map, const uint8_t* codes, const MxOperand& op, uint64_t batch, uint32_t box_lines) {
     const cuuint64_t pitch = (cuuint64_t)op.blocks * 16, dims[3] = {pitch, op.lines, batch}, strides[2] = {pitch, pitch * op.lines};
     const cuuint32_t box[3] = {128, box_lines, 1}, each[3] = {1, 1, 1};
-    const EncodeTiled encode = encode_tiled();
-    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(codes), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(codes), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 // The output in slabs of 32 by 32, where it lies on 16 bytes; false where it does not.
@@ -1177,9 +1185,8 @@ bool mx4_map_output(CUtensorMap* map, float* out, uint64_t m, uint64_t n, uint64
     if ((uintptr_t)out % 16 || ld % 4 || (batch > 1 && batch_stride % 4) || ld >= 1ull << 38 || (batch > 1 && batch_stride >= 1ull << 38)) return false;
     const cuuint64_t dims[3] = {n, m, batch}, strides[2] = {ld * 4, (batch > 1 ? batch_stride : ld) * 4};
     const cuuint32_t box[3] = {32, 32, 1}, each[3] = {1, 1, 1};
-    const EncodeTiled encode = encode_tiled();
-    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, out, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, out, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 } // namespace
