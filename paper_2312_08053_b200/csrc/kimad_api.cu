@@ -1317,6 +1317,8 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
     if (!out_dev || (length && (!a_codes_dev || !a_scales_dev || !b_codes_dev || !b_scales_dev)) || !mx4_apart(m, n, ld, batch, batch_stride))
         return KIMAD_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    // An empty sum is 0 whatever alpha is; with -0 added to it beta out keeps its zeros' signs.
+    if (length == 0) alpha = beta != 0.f ? -1.f : 1.f;
     const MxProduct p{out_dev, ld, batch_stride, a_scales_dev, b_scales_dev, MxOperand((uint32_t)m, (uint32_t)length), MxOperand((uint32_t)n, (uint32_t)length),
                       alpha, beta, status_dev, g_mx4_wait_clocks.load(std::memory_order_relaxed), g_mx4_withhold.load(std::memory_order_relaxed)};
     const uint64_t tiles = (uint64_t)p.a.line_tiles * p.b.line_tiles;

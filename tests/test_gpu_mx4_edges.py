@@ -30,3 +30,15 @@ def test_first_calls_of_a_thread():
     t.join()
     torch.cuda.synchronize()
     assert not failures and torch.equal(out, want) and want.any()
+
+
+@pytest.mark.parametrize("alpha", [float("inf"), float("nan"), -float("inf"), -2.0, 3.0])
+@pytest.mark.parametrize("beta", [0.0, 1.0, -0.5])
+def test_nothing_to_sum_leaves_beta_times_the_output_whatever_alpha(alpha, beta):
+    a, b = kb.Mx4Operand(40, 0, batch=2), kb.Mx4Operand(50, 0, batch=2)
+    was = torch.randn((2, 40, 50), device="cuda")
+    was[0, 0, :2] = torch.tensor([0.0, -0.0])
+    out = was.clone() if beta else torch.full_like(was, float("nan"))
+    kb.kimad_mx4_product(a, b, out, alpha=alpha, beta=beta)
+    want = was * beta if beta else torch.zeros_like(was)
+    assert torch.equal(out.view(torch.int32), want.view(torch.int32))  # bit for bit, zeros' signs too
