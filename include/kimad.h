@@ -286,7 +286,8 @@ int kimad_mx4_read(const kimad_ctx* ctx, const kimad_mx4_message* msg, void* out
  *   (0: the same one).  along 0: blocks run over the rows, the operand has `cols` lines of `rows` values (x is transposed: tokens by
  *   features become features of tokens); along 1: blocks run over the columns, `rows` lines of `cols` values.
  * kimad_mx4_dequantize: back to values, dtype KIMAD_F32 or KIMAD_BF16 (exact in both); blocks of scale 255 read as NaN.  What lies between the rows is left
- *   as it is; matrices of a batch must not overlap.
+ *   as it is.  Matrices of a batch lie apart: behind each other ((rows - 1) ld + cols <= batch_stride), or beside each other, a row of every one before the
+ *   next row of the first (cols <= batch_stride and (batch - 1) batch_stride + cols <= ld: [rows][batch][cols] storage).  Other layouts are refused.
  * rows, cols or batch 0: nothing is done.  Asynchronous on cuda_stream; no context, no workspace.  Errors: INVALID_ARG, CUDA. */
 int kimad_mx4_operand_bytes(uint64_t lines, uint64_t length, uint64_t* code_bytes, uint64_t* scale_bytes);
 int kimad_mx4_quantize(const void* x_dev, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t batch, uint64_t batch_stride, uint32_t along,
@@ -297,7 +298,7 @@ int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, vo
 /* kimad_mx4_product: out <- beta out + alpha A B^T, A an operand of m lines, B one of n lines, both of `length` values: out_ij gets alpha sum_t A_it B_jt.
  * With the two factors of a linear layer's gradient (its inputs and its outputs' gradients, quantised along the tokens: along 0) this is that
  * gradient, summed over the tokens into the layer's place in a flat gradient or estimator vector: out_dev device f32, [batch][m][n], `ld` elements from
- * row to row and batch_stride from matrix to matrix (no two outputs on top of each other), any alignment of elements.  The sum is
+ * row to row and batch_stride from matrix to matrix (outputs apart, as for kimad_mx4_dequantize), any alignment of elements.  The sum is
  * taken in binary32 on the tensor cores (products of codes exactly, at most one rounding per 32 values and addition), always in the same
  * order; then fl32(alpha sum), with beta != 0 fl32(beta out + that) with one rounding; with beta = 0 out is not read.  Blocks of scale 255 make NaN of their
  * line's outputs.  length 0: out <- beta out.  What lies between rows and matrices is left as it is.

@@ -1125,9 +1125,13 @@ bool mx4_operand_ok(uint64_t lines, uint64_t length, uint64_t batch, const void*
     return tiles <= 0x7fffffffull && (tiles == 0 || batch <= 0x7fffffffull / tiles);
 }
 
-// Whether the matrices of a batch of outputs lie apart (whatever their strides).
+// Whether the matrices of a batch of outputs lie apart in one of the two ways that are taken: behind each other, or beside each other with a row of every
+// matrix before the next row of the first one ([rows][batch][cols] storage).
 bool mx4_apart(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t batch, uint64_t batch_stride) {
-    return batch <= 1 || (unsigned __int128)(rows - 1) * ld + cols <= batch_stride;
+    using wide = unsigned __int128;
+    const wide matrix = (wide)(rows - 1) * ld + cols, row = (wide)(batch - 1) * batch_stride + cols; // how far a matrix reaches, and a row of all of them
+    if (matrix >= 1ull << 61 || (batch > 1 && matrix + row >= 1ull << 61)) return false; // no distances in 64 bits
+    return batch <= 1 || matrix <= batch_stride || (cols <= batch_stride && row <= ld);
 }
 
 std::atomic<long long> g_mx4_wait_clocks{kMxWaitClocks}; // kimad_debug_mx4_set_wait_limit

@@ -47,3 +47,11 @@ def test_messages_of_contexts_with_the_same_layers_are_taken():
     msg = kb.Mx4Message(of, device="cpu")
     with pytest.raises(ValueError, match="host memory"):
         kb.kimad_mx4_read(to, msg, torch.zeros((2, 80)))
+
+
+@pytest.mark.parametrize("ld,batch_stride", [(9, 4), (10, 4), (9, 5), (39, 0), (1 << 63, 0), (14, 6), (6, 1), (15, 1 << 63)])
+def test_outputs_on_top_of_each_other_are_refused(ld, batch_stride):
+    """Three matrices of 7 by 5: behind each other they need batch_stride >= 6 ld + 5, beside each other batch_stride >= 5 and ld >= 2 batch_stride + 5."""
+    L, one, zero = kb.load(), C.c_float(1), C.c_float(0)
+    assert L.kimad_mx4_dequantize(512, 1024, 256, 0, 7, 5, ld, 3, batch_stride, 1, None) == BAD
+    assert L.kimad_mx4_product(256, ld, batch_stride, 7, 5, 40, 3, 512, 1024, 2048, 4096, one, zero, None, None) == BAD
