@@ -309,7 +309,8 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
                       const uint8_t* a_scales_dev, const uint8_t* b_codes_dev, const uint8_t* b_scales_dev, float alpha, float beta, int32_t* status_dev,
                       void* cuda_stream);
 
-/* Limit, in SM clocks, of the waits inside the product's kernels, for all calls of the process from now on (default and maximum 2^31, about a second).  For
+/* Limit, in SM clocks, of the waits inside the product's kernels, for all calls of the process from now on (default and maximum 2^31, about a second; waits
+ * for a whole sum have 32 clocks more for every value of it, some fifteen times what it takes).  For
  * tests: with withhold != 0 the kernels do not bring their operands, so that what they wait for never comes and the limit is what ends them;
  * the call sets its status and leaves its outputs as they were.  Errors: INVALID_ARG. */
 int kimad_debug_mx4_set_wait_limit(uint64_t clocks, int withhold);

@@ -11,7 +11,8 @@
 // k_mx4_product_pairs has two SMs for a tile, k_mx4_product_parts several for parts of the summed axis of one.
 // Lines behind the operand's last and bytes behind a line's last block are filled with zeros by TMA: code 0 times any scale that is there
 // is 0, and the scales that are not there are 0 too.
-// Waits are bounded (kMxWaitClocks): a CTA whose wait ran out stores nothing, waits for its copies, frees its tensor memory and sets the status.
+// Waits are bounded (kMxWaitClocks, and kMxRoundClocks a round where a whole sum is waited for): a CTA whose wait ran out stores nothing more, waits for
+// its copies, frees its tensor memory and sets the status.
 #pragma once
 #include <cuda.h> // CUtensorMap
 
@@ -22,6 +23,7 @@ namespace kimad {
 constexpr uint32_t kMxStageK = 256;                  // values of the summed axis in a stage
 constexpr uint32_t kMxOperandStage = 128 * 128;      // bytes of codes of an operand in a stage
 constexpr long long kMxWaitClocks = 1ll << 31;       // about a second: the limit of a wait, by default, and of those after a failure
+constexpr long long kMxRoundClocks = 8192;           // what a wait for a whole sum is given besides, a round of kMxStageK values: they take about 500
 
 // Instruction descriptor of kind mxf4: E2M1 by E2M1, scales UE8M0, K-major, N (bits 17-22, in eights), M (bits 27-28, in 128s).
 // The two scales of a product lie in bytes 0-1 or 2-3 of their column (bits 4-5 for B, 29-30 for A).
@@ -407,7 +409,7 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if (slab % parts != part)
                     far_copy(shared_of(in + 4096 * (part * (4 / parts) + slab / parts), slab % parts), out + 4096 * slab, 4096, shared_of(joined, slab % parts));
         }
-        fine = mbar_wait(joined, 0, wait);
+        fine = mbar_wait(joined, 0, MxWait{&s_failed, p.wait_clocks + (long long)most * kMxRoundClocks}); // (the other CTAs may have started later)
         __syncwarp();
     }
     if (warp < 4 && fine) {
@@ -537,6 +539,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 
     const uint32_t pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     const uint32_t rounds = (p.a.blocks + kMxStageK / kMxBlock - 1) / (kMxStageK / kMxBlock), tiles = p.a.block_tiles;
+    const MxWait whole{&s_failed, p.wait_clocks + (long long)rounds * kMxRoundClocks};
     uint32_t it = 0; // stages whose copies, or whose products, have been issued
     MxRing<S> q;
     if (warp == 12) {
@@ -649,7 +652,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 for (uint32_t i = 0; i < SLABS; ++i)
                     if (i < mine) ask(i);
             }
-            if (!mbar_wait(done + 8 * u.s, u.parity, wait) || wait.failed()) break;
+            if (!mbar_wait(done + 8 * u.s, u.parity, whole) || wait.failed()) break;
             __syncwarp();
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
