@@ -57,7 +57,7 @@ extern "C" {
 #define KIMAD_ERR_WORKSPACE (-2) /* workspace missing, too small or misaligned                        */
 #define KIMAD_ERR_CAPACITY (-3)  /* a worker selected more entries than max_packed_elems             */
 #define KIMAD_ERR_NONFINITE (-4) /* Inf/NaN met in grad - g (only reported when check_finite != 0)   */
-#define KIMAD_ERR_TIMEOUT (-5)   /* in stats: a bounded wait inside the knapsack kernel ran out      */
+#define KIMAD_ERR_TIMEOUT (-5)   /* a bounded wait inside the knapsack (in stats) or the product (its status) ran out */
 #define KIMAD_ERR_CUDA (-6)      /* a CUDA runtime call failed                                       */
 #define KIMAD_ERR_NOMEM (-7)     /* host allocation failed                                           */
 #define KIMAD_ERR_TOO_LARGE (-8) /* kimad_step_builtin_scratch: scratch need above the built-in array */
@@ -302,12 +302,18 @@ int kimad_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, vo
  * taken in binary32 on the tensor cores (products of codes exactly, at most one rounding per 32 values and addition), always in the same
  * order; then fl32(alpha sum), with beta != 0 fl32(beta out + that) with one rounding; with beta = 0 out is not read.  Blocks of scale 255 make NaN of their
  * line's outputs.  length 0: out <- beta out.  What lies between rows and matrices is left as it is.
- * status_dev: device i32 or NULL; set to KIMAD_ERR_TIMEOUT if a bounded wait inside the kernel ran out (some outputs are then left as they were), else left
- * as it is.
+ * status_dev: device i32 or NULL; set to KIMAD_ERR_TIMEOUT if a bounded wait inside the kernel ran out, else left as it is.  Some outputs are then written
+ * and some left as they were: with beta != 0 out has to be made anew before the call is repeated.  Whether or not there is a status_dev, the
+ * device's status is set too (kimad_mx4_product_status).
  * Asynchronous on cuda_stream; no context, no workspace.  m, n or batch 0: nothing is done.  Errors: INVALID_ARG, CUDA. */
 int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64_t m, uint64_t n, uint64_t length, uint64_t batch, const uint8_t* a_codes_dev,
                       const uint8_t* a_scales_dev, const uint8_t* b_codes_dev, const uint8_t* b_scales_dev, float alpha, float beta, int32_t* status_dev,
                       void* cuda_stream);
+
+/* KIMAD_ERR_TIMEOUT if a bounded wait ran out in any product on the current device since the status was last reset, else KIMAD_OK: to be asked where a
+ * result leaves the device, once for all products before it.  Waits for cuda_stream (products on other streams are covered as far as they are done by
+ * then); reset != 0 sets the status back.  Not on a stream that is being captured.  Errors: INVALID_ARG, CUDA. */
+int kimad_mx4_product_status(int reset, void* cuda_stream);
 
 /* Limit, in SM clocks, of the waits inside the product's kernels, for all calls of the process from now on (default and maximum 2^31, about a second; waits
  * for a whole sum have 32 clocks more for every value of it, some fifteen times what it takes).  For

@@ -149,6 +149,8 @@ def load():
     L.kimad_debug_mx4_set_wait_limit.argtypes = [u64, C.c_int]
     L.kimad_mx4_product.restype = C.c_int
     L.kimad_mx4_product.argtypes = [vp] + [u64] * 6 + [vp] * 4 + [C.c_float, C.c_float, vp, vp]
+    L.kimad_mx4_product_status.restype = C.c_int
+    L.kimad_mx4_product_status.argtypes = [C.c_int, vp]
     L.kimad_monitor_create.restype = C.c_int
     L.kimad_monitor_create.argtypes = [C.POINTER(vp), u32, dbl]
     L.kimad_monitor_destroy.restype = None
@@ -629,7 +631,7 @@ def kimad_mx4_dequantize(op: Mx4Operand, out, along: int, stream=None) -> None:
 
 def kimad_mx4_product(a: Mx4Operand, b: Mx4Operand, out, alpha=1.0, beta=0.0, status=None, stream=None) -> None:
     """out <- beta out + alpha a b^T.  out: CUDA float32 [a.lines][b.lines] or [batch][a.lines][b.lines], rows of consecutive elements at any stride
-    and place; status: CUDA int32 tensor of one element or None."""
+    and place; status: CUDA int32 tensor of one element or None (kimad_mx4_product_status tells of all products of the device)."""
     _mx4_dtype(out, "out", KIMAD_F32)
     if a.length != b.length or a.batch != b.batch:
         raise ValueError(f"kimad_mx4_product: operands of {a.batch} x {a.length} and of {b.batch} x {b.length}")
@@ -641,6 +643,13 @@ def kimad_mx4_product(a: Mx4Operand, b: Mx4Operand, out, alpha=1.0, beta=0.0, st
         _mx4_stream("kimad_mx4_product", stream, status.get_device())
     _check((_lib or load()).kimad_mx4_product(out.data_ptr(), ld, bs, a.lines, b.lines, a.length, a.batch, a.codes_ptr, a.scales_ptr,
                                     b.codes_ptr, b.scales_ptr, alpha, beta, None if status is None else status.data_ptr(), s), "kimad_mx4_product")
+
+
+def kimad_mx4_product_status(reset: bool = False, stream=None) -> int:
+    """KIMAD_ERR_TIMEOUT if a bounded wait ran out in a product on the current device since the last reset, else KIMAD_OK.  Waits for the stream; to be asked
+    before the results of products are relied on."""
+    st = load().kimad_mx4_product_status(int(bool(reset)), _stream_ptr(stream))
+    return st if st == KIMAD_ERR_TIMEOUT else _check(st, "kimad_mx4_product_status")
 
 
 def kimad_debug_mx4_set_wait_limit(clocks: int, withhold: bool = False) -> None:

@@ -1354,6 +1354,23 @@ int kimad_mx4_product(float* out_dev, uint64_t ld, uint64_t batch_stride, uint64
     return KIMAD_OK;
 }
 
+int kimad_mx4_product_status(int reset, void* cuda_stream) {
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    CUDA_TRY(cudaStreamIsCapturing(s, &capturing));
+    if (capturing != cudaStreamCaptureStatusNone) return KIMAD_ERR_INVALID_ARG;
+    void* at = nullptr;
+    int32_t status = KIMAD_OK;
+    CUDA_TRY(cudaGetSymbolAddress(&at, g_mx4_status));
+    CUDA_TRY(cudaMemcpyAsync(&status, at, sizeof(status), cudaMemcpyDeviceToHost, s));
+    CUDA_TRY(cudaStreamSynchronize(s));
+    if (reset && status != KIMAD_OK) {
+        CUDA_TRY(cudaMemsetAsync(at, 0, sizeof(status), s));
+        CUDA_TRY(cudaStreamSynchronize(s));
+    }
+    return status;
+}
+
 int kimad_debug_mx4_set_wait_limit(uint64_t clocks, int withhold) {
     if (clocks > (uint64_t)kMxWaitClocks) return KIMAD_ERR_INVALID_ARG;
     g_mx4_wait_clocks.store((long long)clocks, std::memory_order_relaxed);

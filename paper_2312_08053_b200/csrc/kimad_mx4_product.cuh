@@ -12,7 +12,7 @@
 // Lines behind the operand's last and bytes behind a line's last block are filled with zeros by TMA: code 0 times any scale that is there
 // is 0, and the scales that are not there are 0 too.
 // Waits are bounded (kMxWaitClocks, and kMxRoundClocks a round where a whole sum is waited for): a CTA whose wait ran out stores nothing more, waits for
-// its copies, frees its tensor memory and sets the status.
+// its copies, frees its tensor memory and sets the device's status, and the caller's if there is one.
 #pragma once
 #include <cuda.h> // CUtensorMap
 
@@ -134,6 +134,12 @@ template <uint32_t N> struct MxRing {
         if (++s == N) { s = 0; parity ^= 1u; }
     }
 };
+
+__device__ int32_t g_mx4_status; // KIMAD_ERR_TIMEOUT once a wait of any product has run out on the device (kimad_mx4_product_status)
+__device__ __forceinline__ void mx_report(int32_t* status) {
+    g_mx4_status = KIMAD_ERR_TIMEOUT;
+    if (status) *status = KIMAD_ERR_TIMEOUT;
+}
 
 struct MxProduct {
     float* out;
@@ -432,7 +438,7 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (s_failed) { // what was issued still writes to this CTA's shared and tensor memory
-        if (threadIdx.x == 0 && p.status) *p.status = KIMAD_ERR_TIMEOUT;
+        if (threadIdx.x == 0) mx_report(p.status);
         const long long began = clock64();
         if (warp == 4 && lane == 0)
             for (uint32_t i = r > S ? r - S : 0; i < r; ++i)
@@ -707,7 +713,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     }
     __syncthreads();
     if (s_failed) { // what was issued still writes to the pair's shared and tensor memory
-        if (threadIdx.x == 0 && p.status) *p.status = KIMAD_ERR_TIMEOUT;
+        if (threadIdx.x == 0) mx_report(p.status);
         const long long began = clock64();
         if (warp == 12 && lane == 0 && rank == 0) // (the second CTA may be S stages ahead; a stage that only one has issued does not end, but its copies do within the limit)
             for (uint32_t i = it > S ? it - S : 0; i < it + S && !p.withhold; ++i)

@@ -29,3 +29,46 @@ def test_the_limit_grows_with_the_sum(limit, m, n, length):
     kb.kimad_mx4_product(a, b, out, status=status)
     torch.cuda.synchronize()
     assert int(status) == 0 and (out == float(length)).all()
+
+
+@pytest.mark.parametrize("m,n,length", [(300, 200, 64), (128, 128, 8192)])
+def test_a_product_without_a_status_of_its_own_is_not_silent(limit, m, n, length):
+    """The operands are withheld, by pairs and by parts: the device's status says so until it is reset."""
+    a, b, out = ones(m, length), ones(n, length), torch.zeros((m, n), device="cuda")
+    assert kb.kimad_mx4_product_status(reset=True) == 0
+    kb.kimad_mx4_product(a, b, out)
+    assert kb.kimad_mx4_product_status() == 0 and (out == float(length)).all()
+    limit(200000, withhold=True)
+    kb.kimad_mx4_product(a, b, out, beta=1.0)
+    limit(1 << 31)
+    kb.kimad_mx4_product(a, b, out, beta=1.0)  # a call that is right does not cover it up
+    assert kb.kimad_mx4_product_status() == kb.KIMAD_ERR_TIMEOUT
+    assert kb.kimad_mx4_product_status(reset=True) == kb.KIMAD_ERR_TIMEOUT
+    assert kb.kimad_mx4_product_status() == 0
+    assert (out == 2.0 * length).all()
+
+
+def test_a_captured_product_reports_when_it_is_replayed(limit):
+    a, out = ones(40, 64), torch.zeros((40, 40), device="cuda")
+    kb.kimad_mx4_product_status(reset=True)
+    limit(200000, withhold=True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kb.kimad_mx4_product(a, a, out)
+        with pytest.raises(kb.KimadError) as e:  # nothing could be waited for here; the capture goes on
+            kb.kimad_mx4_product_status()
+        assert e.value.code == kb.KIMAD_ERR_INVALID_ARG
+    limit(1 << 31)
+    assert kb.kimad_mx4_product_status() == 0
+    for _ in range(2):
+        graph.replay()
+        assert kb.kimad_mx4_product_status(reset=True) == kb.KIMAD_ERR_TIMEOUT
+
+
+def test_the_status_can_be_read_on_another_stream(limit):
+    a, out, side = ones(40, 64), torch.zeros((40, 40), device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    kb.kimad_mx4_product_status(reset=True)
+    limit(200000, withhold=True)
+    kb.kimad_mx4_product(a, a, out, stream=side)
+    assert kb.kimad_mx4_product_status(reset=True, stream=side) == kb.KIMAD_ERR_TIMEOUT
