@@ -17,7 +17,8 @@
 // 2 a work list (exact path, recount) appended beyond its capacity; 3 write sweep: packed position beyond the capacity or element
 // outside its chunk; 4 knapsack: a record, row or exchange outside the memory it lies in; 5 knapsack: a cell outside its row;
 // 6 selection: a listed entry outside its layer's chunks; 7 curve: the pieces of a refined bin do not add up to the bin; 8 4-bit message: a block
-// behind the buffers' end.
+// behind the buffers' end; 9 4-bit operand: a block's codes or scale behind its matrix's end; 10 product: an operand's scales or an output behind its
+// matrix's end.
 // In the ordinary build KIMAD_CHECK(cond, bit) is `true`.
 #if defined(KIMAD_CHECKED) && defined(__CUDACC__)
 __device__ unsigned int g_kimad_check_word;

@@ -186,6 +186,7 @@ struct MxMessage {
     uint64_t code_bytes, scale_bytes; // of a worker
     __device__ __forceinline__ uint32_t* words(uint32_t w, uint64_t first) const { return reinterpret_cast<uint32_t*>(codes + (size_t)w * code_bytes) + first * 4; }
     __device__ __forceinline__ uint8_t* bytes(uint32_t w, uint64_t first) const { return scales + (size_t)w * scale_bytes + first; }
+    __device__ __forceinline__ bool holds(uint64_t first, uint32_t blocks) const { return (first + blocks) * 16 <= code_bytes && first + blocks <= scale_bytes; }
 };
 
 // Eight blocks of a pass: values, message, estimator.  `blocks` of them are there.
@@ -354,7 +355,7 @@ k_mx4_step(const T* __restrict__ grads, float* __restrict__ state, uint64_t stri
     uint32_t absent = 0;
     for (uint32_t b = (piece * kMxWarps + warp) * kMxGroup; b < sp.blocks; b += pieces * kMxWarps * kMxGroup) {
         const uint32_t e = b * kMxBlock, lim = min(sp.left - e, kMxGroupElems), blocks = min(sp.blocks - b, kMxGroup);
-        if (!KIMAD_CHECK((sp.first + b + blocks) * 16 <= msg.code_bytes && sp.first + b + blocks <= msg.scale_bytes, 8)) break;
+        if (!KIMAD_CHECK(msg.holds(sp.first + b, blocks), 8)) break;
         if (aligned && lim == kMxGroupElems) mx_step_group<true>(g + e, at + e, lim, lane, blocks, words + b * 4, bytes + b, nullptr, err, absent);
         else mx_step_group<false>(g + e, at + e, lim, lane, blocks, words + b * 4, bytes + b, s_buf[warp], err, absent);
     }
@@ -449,6 +450,7 @@ k_mx4_apply(MxMessage msg, const Chunk* __restrict__ chunks, const LayerDesc* __
     const bool aligned = mx_aligned8(at + (size_t)m_first * stride) && (!MODEL || (mx_aligned8(xa) && (W == 1 || stride % 8 == 0)));
     for (uint32_t b = (piece * kMxWarps + warp) * kMxGroup; b < sp.blocks; b += pieces * kMxWarps * kMxGroup) {
         const uint32_t e = b * kMxBlock, lim = min(sp.left - e, kMxGroupElems), blocks = min(sp.blocks - b, kMxGroup);
+        if (!KIMAD_CHECK(msg.holds(sp.first + b, blocks), 8)) break;
         if (aligned && lim == kMxGroupElems)
             mx_apply_group<true, MODEL>(msg, sp.first + b, at + e, stride, xa + (MODEL ? e : 0), lim, lane, blocks, m_first, m_end, wt, gamma, nullptr);
         else mx_apply_group<false, MODEL>(msg, sp.first + b, at + e, stride, xa + (MODEL ? e : 0), lim, lane, blocks, m_first, m_end, wt, gamma, s_buf[warp]);
@@ -473,6 +475,7 @@ k_mx4_read(MxMessage msg, const Chunk* __restrict__ chunks, const LayerDesc* __r
     const uint32_t step = pieces * kMxWarps * kMxGroup;
     for (uint32_t b0 = (piece * kMxWarps + warp) * kMxGroup; b0 < sp.blocks; b0 += U * step) {
         uint32_t word[U], byte[U];
+        if (!KIMAD_CHECK(msg.holds(sp.first, sp.blocks), 8)) break;
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
             const uint32_t b = b0 + u * step;
@@ -505,6 +508,9 @@ struct MxOperand {
           block_tiles((blocks + 3) / 4) {}
     KIMAD_HD uint64_t code_bytes() const { return (uint64_t)lines * blocks * 16; }
     KIMAD_HD uint64_t scale_bytes() const { return (uint64_t)line_tiles * block_tiles * 512; }
+    __device__ __forceinline__ bool holds(uint32_t line, uint32_t block) const {
+        return ((uint64_t)line * blocks + block + 1) * 16 <= code_bytes() && scale_word(line, block / 4) * 4 + block % 4 < scale_bytes();
+    }
     // the four scales of a line in a tile of blocks, as a word
     KIMAD_HD uint64_t scale_word(uint32_t line, uint32_t tile) const {
         return ((uint64_t)(line / kMxTile) * block_tiles + tile) * 128 + (line % 32) * 4 + line % kMxTile / 32;
@@ -550,7 +556,7 @@ k_mx4_quantize_rows(const T* __restrict__ x, uint64_t ld, uint64_t batch_stride,
         const uint32_t own = b0 + i * kMxGroup + lane / 4;
         uint32_t byte;
         const uint32_t word = mx_quantize8(v[i], byte);
-        if (line < op.lines && own < op.blocks) words[i * 32 + lane] = word;
+        if (line < op.lines && own < op.blocks && KIMAD_CHECK(op.holds(line, own), 9)) words[i * 32 + lane] = word;
         if (lane % 4 == 0 && own < op.block_tiles * 4) tiles[op.scale_word(line, own / 4) * 4 + own % 4] = (uint8_t)byte;
     }
 }
@@ -638,7 +644,7 @@ k_mx4_quantize_cols(const T* __restrict__ x, uint64_t ld, uint64_t batch_stride,
 #pragma unroll
     for (uint32_t i = threadIdx.x; i < kMxTile * 4; i += kThreads) {
         const uint32_t out = lt * kMxTile + i / 4, block = bt * 4 + i % 4;
-        if (out < op.lines && block < op.blocks) reinterpret_cast<uint4*>(codes)[(n * op.lines + out) * op.blocks + block] = s_codes[i / 4][i % 4];
+        if (out < op.lines && block < op.blocks && KIMAD_CHECK(op.holds(out, block), 9)) reinterpret_cast<uint4*>(codes)[(n * op.lines + out) * op.blocks + block] = s_codes[i / 4][i % 4];
     }
     if (threadIdx.x < 128)
         reinterpret_cast<uint32_t*>(scales)[((n * op.line_tiles + lt) * op.block_tiles + bt) * 128 + threadIdx.x] = reinterpret_cast<uint32_t*>(s_scales)[threadIdx.x];
@@ -666,8 +672,9 @@ k_mx4_dequantize_rows(T* __restrict__ x, uint64_t ld, uint64_t batch_stride, MxO
 #pragma unroll
     for (uint32_t i = 0; i < kMxRowGroups; ++i) {
         const uint32_t own = b0 + i * kMxGroup + lane / 4;
-        word[i] = own < op.blocks ? __ldcs(words + i * 32 + lane) : 0u;
-        byte[i] = own < op.blocks ? (uint32_t)tiles[op.scale_word(line, own / 4) * 4 + own % 4] : 0u;
+        const bool here = own < op.blocks && KIMAD_CHECK(op.holds(line, own), 9);
+        word[i] = here ? __ldcs(words + i * 32 + lane) : 0u;
+        byte[i] = here ? (uint32_t)tiles[op.scale_word(line, own / 4) * 4 + own % 4] : 0u;
     }
 #pragma unroll
     for (uint32_t i = 0; i < kMxRowGroups; ++i) {
@@ -702,7 +709,7 @@ k_mx4_dequantize_cols(T* __restrict__ x, uint64_t ld, uint64_t batch_stride, MxO
 #pragma unroll
     for (uint32_t i = threadIdx.x; i < kMxTile * 4; i += kThreads) {
         const uint32_t in = lt * kMxTile + i / 4, block = bt * 4 + i % 4;
-        if (in < op.lines && block < op.blocks) s_codes[i / 4][i % 4] = __ldcs(reinterpret_cast<const uint4*>(codes) + (n * op.lines + in) * op.blocks + block);
+        if (in < op.lines && block < op.blocks && KIMAD_CHECK(op.holds(in, block), 9)) s_codes[i / 4][i % 4] = __ldcs(reinterpret_cast<const uint4*>(codes) + (n * op.lines + in) * op.blocks + block);
     }
     if (threadIdx.x < 128) s_scales[threadIdx.x] = __ldcs(reinterpret_cast<const uint32_t*>(scales) + ((n * op.line_tiles + lt) * op.block_tiles + bt) * 128 + threadIdx.x);
     __syncthreads();

@@ -168,6 +168,7 @@ struct MxOutput {
         mine = at + lane * ld;
         rows = row < p.a.lines ? min(p.a.lines - row, 32u) : 0u;
         cols = col < p.b.lines ? min(p.b.lines - col, most_cols) : 0u;
+        if (!KIMAD_CHECK(rows == 0 || cols == 0 || ((uint64_t)row + rows <= p.a.lines && (uint64_t)col + cols <= p.b.lines && p.b.lines <= ld), 10)) rows = cols = 0;
         aligned = reinterpret_cast<uintptr_t>(at) % 32 == 0 && ld % 8 == 0;
     }
     __device__ __forceinline__ bool whole(uint32_t slab) const { return aligned && 32 * slab + 32 <= cols; }
@@ -571,6 +572,7 @@ k_mx4_product_pairs(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             const uint8_t* sb = p.scales_b + ((uint64_t)t.n * p.b.line_tiles + lb) * tiles * 512;
             for (uint32_t r = 0; r < rounds; ++r, ++it, q.next()) {
                 const uint32_t to = smem + q.s * kMxPairStageBytes + kMxOperandStage + kMxPairBytesB, here = full + 8 * q.s;
+                if (!KIMAD_CHECK(2 * r < tiles && lb + have_b < p.b.line_tiles && la < p.a.line_tiles + !have_a, 10)) { s_failed = 1; break; }
                 if (it >= S && !mbar_wait(empty + 8 * q.s, q.parity ^ 1u, wait)) break;
                 if (one_lane()) {
                     const uint32_t bytes = min(tiles - 2 * r, 2u) * 512u;

@@ -35,7 +35,7 @@ def test_the_limit_grows_with_the_sum(limit, m, n, length):
 def test_a_product_without_a_status_of_its_own_is_not_silent(limit, m, n, length):
     """The operands are withheld, by pairs and by parts: the device's status says so until it is reset."""
     a, b, out = ones(m, length), ones(n, length), torch.zeros((m, n), device="cuda")
-    assert kb.kimad_mx4_product_status(reset=True) == 0
+    kb.kimad_mx4_product_status(reset=True)  # (what tests before this one have left)
     kb.kimad_mx4_product(a, b, out)
     assert kb.kimad_mx4_product_status() == 0 and (out == float(length)).all()
     limit(200000, withhold=True)
