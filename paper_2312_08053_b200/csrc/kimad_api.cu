@@ -1184,9 +1184,10 @@ bool mx4_map(CUtensorMap* map, const uint8_t* codes, const MxOperand& op, uint64
                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
-// The output in slabs of 32 by 32, where it lies on 16 bytes; false where it does not.
+// The output in slabs of 32 by 32, where it and its rows lie on 16 bytes and are whole pieces of 16 bytes; false where they are not.  (A store cuts a row off
+// at the 16 bytes that its last element lies in: the elements between rows that share them would be written over.)
 bool mx4_map_output(CUtensorMap* map, float* out, uint64_t m, uint64_t n, uint64_t batch, uint64_t ld, uint64_t batch_stride) {
-    if ((uintptr_t)out % 16 || ld % 4 || (batch > 1 && batch_stride % 4) || ld >= 1ull << 38 || (batch > 1 && batch_stride >= 1ull << 38)) return false;
+    if ((uintptr_t)out % 16 || n % 4 || ld % 4 || (batch > 1 && batch_stride % 4) || ld >= 1ull << 38 || (batch > 1 && batch_stride >= 1ull << 38)) return false;
     const cuuint64_t dims[3] = {n, m, batch}, strides[2] = {ld * 4, (batch > 1 ? batch_stride : ld) * 4};
     const cuuint32_t box[3] = {32, 32, 1}, each[3] = {1, 1, 1};
     return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, out, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
