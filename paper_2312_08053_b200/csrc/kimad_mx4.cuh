@@ -319,7 +319,7 @@ __device__ __forceinline__ void mx_stats(const MxStats& st, const LayerDesc* lay
 }
 
 // Where the CTAs are few, the last one of a worker does that: the pass of a small model then is one launch (0.10 M elements: 4.5 us of the host's time instead of
-// 6.3).  Where they are many, a kernel of its own behind them: their arrivals and the smaller CTA cost more there (2 x 25.6 M elements 285 us instead of 277).
+// 6.3).  Where they are many, a kernel of its own behind them: their arrivals and the smaller CTA cost more there (124 M elements in odd layers 285 us instead of 277).
 constexpr uint32_t kMxStatsThreads = 1024;
 __global__ void __launch_bounds__(kMxStatsThreads)
 k_mx4_stats(MxStats st, const LayerDesc* __restrict__ layers, uint32_t ctas, uint32_t log_pieces) {
@@ -564,7 +564,8 @@ k_mx4_quantize_rows(const T* __restrict__ x, uint64_t ld, uint64_t batch_stride,
 // Blocks along the other axis, which transposes: a CTA takes 128 lines (columns of x) by 128 values (rows), a lane one block of each of two
 // neighbouring columns.  Rows are read in whole lines and a block's values need no exchange between lanes; codes go through shared memory so that 64
 // bytes of a line are written together.  Pairs of columns are read as one where they are aligned and the tile is whole.
-// (One column per lane and 16-bit loads, 28 instructions per value: 8192 x 5632 bfloat16 values 133 us, 27 this way.)
+// (One column per lane and 16-bit loads, 28 instructions per value: 8192 x 5632 bfloat16 values 133 us, 27 this way.  Lanes write and read their codes 128
+// bytes apart, so that eight of them meet in four banks: half of the shared memory's cycles, here and on the way back, beside HBM's.)
 template <typename T> struct MxPair;
 template <> struct MxPair<float> {
     float2 v;

@@ -461,7 +461,7 @@ k_mx4_product_parts(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // B's in shared memory, and both tensor cores read both halves.  An SM then reads 28 KB of codes per 256 values of a tile of 128 by 192 sums, where 128 by
 // 128 alone needs 32: an SM takes 64 bytes per clock from L2, so a tile alone runs at half the products' rate at most.
 // One CTA per SM stays for all its tiles; the sums are held twice, so that one tile's outputs are written beside the next one's products.  Outputs
-// on 16 bytes come and go by TMA, slab by slab: the stores of eight warps are more than an SM gets rid of at once (about 16 bytes per clock when all
+// on 16 bytes (place, row distance and row length) come and go by TMA, slab by slab: the stores of eight warps are more than an SM gets rid of at once (about 16 bytes per clock when all
 // write), and what waits in line behind them are the other warps' barriers, scales and products (stages took 2000 clocks beside them, 480 otherwise).
 // Warps: 0-7 outputs (a quarter of the lines and half of the columns each), 8-11 scales to tensor memory, 12 copies of codes, 14 of scales (a copy takes
 // almost 100 clocks to issue; all five of a stage in one warp are more than its products take), 13 products (in the pair's first CTA).
